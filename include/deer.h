@@ -189,6 +189,85 @@ int deer_set_bonus_token(deer_ctx *c, int enable);
 int deer_destroy(deer_ctx *c);
 const char *deer_last_error(const deer_ctx *c); /* c may be NULL: last init-time error */
 
+/* ---- paged 8-bit KV cache -------------------------------------------------------------------
+ *
+ * A cache of one model's keys and values in pages of DEER_KV8_PAGE tokens.  A complete page is kept in e4m3, with one power-of-two
+ * scale per layer and kv head for its keys and one for its values (the smallest that brings the page's largest magnitude to at
+ * most 448); the pages come from one pool through a block table that the GPU builds from the requests' lengths.  The last pages of a
+ * sequence are also held in bf16.  A row reads the pages before its own in 8 bits, and its own page, that of the last key it
+ * sees, in bf16: what it reads depends on positions alone, so that a block of rows equals the same rows one by one, a prompt its
+ * tokens one by one, and rejected drafts leave no trace.
+ *
+ * Per pass: deer_kv8_reserve (tables), then for each layer deer_kv8_append and deer_kv8_attend.  All work is enqueued on the
+ * handle's stream, only deer_kv8_init, _status and _destroy wait; nothing is allocated, and the calls of a pass may be captured into
+ * a graph.  A handle is used by one thread at a time, and its cache and workspace belong to it alone.  Kernels check every page
+ * number and position that they read from device memory. */
+#define DEER_KV8_PAGE 64
+
+typedef struct deer_kv8 deer_kv8;
+
+typedef struct {
+    uint32_t struct_size;   /* sizeof(deer_kv8_params) */
+    uint32_t abi_version;   /* DEER_ABI_VERSION */
+    int32_t n_layers, n_q_heads, n_kv_heads, head_dim;   /* head_dim 32, 64 or 128; up to 64 query heads per kv head */
+    int32_t max_batch;      /* sequences, 1..1024                                                 */
+    int32_t max_seq;        /* tokens per sequence: a multiple of 64, at most 2^20                */
+    int32_t n_pages;        /* pages of the pool; 0: max_batch * max_seq / 64                     */
+    int32_t max_rows;       /* rows of a pass, all sequences together, 1..2^20                    */
+    int32_t device;         /* HIP device ordinal                                                 */
+    void *hip_stream;       /* hipStream_t, default priority; NULL = the default stream           */
+} deer_kv8_params;
+
+/* Bytes the caller must provide, 256-byte aligned: the cache itself, and what a pass works with. */
+typedef struct { size_t cache, workspace; } deer_kv8_sizes;
+
+int deer_kv8_query_sizes(const deer_kv8_params *p, deer_kv8_sizes *out);
+
+/* Creates a handle over caller-owned device buffers, which stay alive until deer_kv8_destroy; no sequence holds any token.
+ * *out is NULL on failure. */
+int deer_kv8_init(const deer_kv8_params *p, void *cache_dev, void *workspace_dev, const deer_kv8_sizes *buf_sizes, deer_kv8 **out);
+
+/* The tables of a pass.  Sequence b < batch keeps its first start_dev[b] tokens (0: none; fewer than it holds: the others are
+ * dropped) and takes new_dev[b] rows at positions start_dev[b] ..; it then holds the pages of start + new tokens, others go back to
+ * the pool.  The rows of the pass are those of sequence 0, then 1, ..  Other sequences keep what they hold.
+ * Host bounds, for launch shapes: rows >= the sum of new_dev, max_new >= its largest, max_len >= the largest start + new.
+ * Refused, one by one and on the device (deer_kv8_status): a sequence with numbers outside these bounds, with start beyond its
+ * tokens, or with a start inside a page whose bf16 rows are gone; and, in order of sequence, the first that the free pages do not
+ * suffice for with every later one that needs any.  Never gone are: the start of its last pass that had rows, every start behind it
+ * if that had at most 64, else every start in its last two pages; and a multiple of 64 needs none.
+ * A refused sequence keeps its tokens and pages; its rows have slot -1, are not appended and come out of deer_kv8_attend as zeros
+ * (of more than max_new rows the first max_new).
+ * Free pages are a stack: pages given back by this call are taken first, in order of sequence and block, then the top. */
+int deer_kv8_reserve(deer_kv8 *c, int32_t batch, const int32_t *start_dev, const int32_t *new_dev, int32_t rows, int32_t max_new, int32_t max_len);
+
+/* The pass's rows of one layer, [rows][n_kv_heads][head_dim], enter the cache: F32 (rounded to bf16, nearest even) or BF16; strides
+ * between rows in elements (a slice of a fused projection is fine), addresses and strides multiples of 16 bytes.  Pages that the
+ * rows complete are quantised.  A row with an infinity or NaN in a head makes every row that sees it NaN there, and no other. */
+int deer_kv8_append(deer_kv8 *c, int32_t layer, const void *k_dev, const void *v_dev, int dtype, int64_t k_stride, int64_t v_stride, int32_t rows);
+
+/* Attention of the pass's rows q [rows][n_q_heads][head_dim] over one layer, behind its deer_kv8_append: out = softmax(scale q K^T) V,
+ * query head h with kv head h / (n_q_heads / n_kv_heads).  limits_dev[row]: how many of its sequence's keys a row sees, from the first
+ * (cut to 0 .. the tokens held; 0: the result is zeros); NULL: its position + 1 (causal).  scale 0: 1 / sqrt(head_dim).  dtype is that
+ * of q and out, F32 (computed to about 2^-22) or BF16; softmax and sums are in fp32.  Rows may be read as often as wanted. */
+int deer_kv8_attend(deer_kv8 *c, int32_t layer, const void *q_dev, int dtype, int64_t q_stride, const int32_t *limits_dev, float scale, void *out_dev,
+                    int64_t out_stride, int32_t rows);
+
+/* Rows of one layer as the cache holds them, [n][n_kv_heads][head_dim], for n (sequence, position) pairs: what 8 bits stand for in
+ * complete pages, else bf16; zeros for a pair that names no token. */
+int deer_kv8_read(deer_kv8 *c, int32_t layer, const int32_t *seq_dev, const int32_t *pos_dev, int32_t n, void *k_dev, void *v_dev, int dtype);
+
+/* Free pages, and the sequences that the last deer_kv8_reserve refused.  Waits for the stream. */
+int deer_kv8_status(deer_kv8 *c, int32_t *free_pages, int32_t *refused);
+
+/* Device addresses of the tables: block_table[max_batch][max_blocks] (-1 beyond a sequence's pages), tokens and pages per sequence;
+ * of the last pass: first row of every sequence [batch + 1], and per row its slot (64 * page + offset; -1: refused or no such row),
+ * sequence and position.  To be read on the handle's stream, and not written. */
+typedef struct { const int32_t *block_table, *lengths, *pages_held, *row_offsets, *slots, *row_seq, *row_pos; int32_t max_blocks; } deer_kv8_tables;
+int deer_kv8_get_tables(const deer_kv8 *c, deer_kv8_tables *out);
+
+int deer_kv8_destroy(deer_kv8 *c);
+const char *deer_kv8_last_error(const deer_kv8 *c);   /* c may be NULL: last failed query or init */
+
 /* ---- inspection surface used by tests and the benchmark (not part of the timed path) -------- */
 
 /* Copies the last pass's logits [batch][k][vocab] (fp32) of `model` to host; needs keep_logits

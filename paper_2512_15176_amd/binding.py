@@ -20,7 +20,8 @@ EXPORTS = ["deer_query_sizes", "deer_init_models", "deer_load_tensor", "deer_pre
            "deer_debug_profile_read", "deer_debug_force_commit", "deer_debug_load_kv", "deer_set_bonus_token",
            "deer_draft_block_multipass", "deer_debug_gemm_tiled", "deer_debug_gemm_block",
            "deer_debug_gemm_stamps", "deer_debug_experts_streamed", "deer_debug_route_spread",
-           "deer_debug_stream_read"]
+           "deer_debug_stream_read", "deer_kv8_query_sizes", "deer_kv8_init", "deer_kv8_reserve", "deer_kv8_append", "deer_kv8_attend",
+           "deer_kv8_read", "deer_kv8_status", "deer_kv8_get_tables", "deer_kv8_destroy", "deer_kv8_last_error"]
 
 
 class DeerError(RuntimeError):
@@ -51,6 +52,21 @@ class Buffers(C.Structure):
 class KvLayout(C.Structure):
     _fields_ = [("k_base", C.c_size_t), ("v_base", C.c_size_t), ("layer_stride", C.c_size_t), ("seq_stride", C.c_size_t),
                 ("head_stride", C.c_size_t), ("max_seq", C.c_int32), ("head_dim", C.c_int32)]
+
+
+class Kv8Params(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("abi_version", C.c_uint32)] + [
+        (n, C.c_int32) for n in ("n_layers", "n_q_heads", "n_kv_heads", "head_dim", "max_batch", "max_seq", "n_pages", "max_rows", "device")] + [
+        ("hip_stream", C.c_void_p)]
+
+
+class Kv8Sizes(C.Structure):
+    _fields_ = [("cache", C.c_size_t), ("workspace", C.c_size_t)]
+
+
+class Kv8Tables(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("block_table", "lengths", "pages_held", "row_offsets", "slots", "row_seq", "row_pos")] + [
+        ("max_blocks", C.c_int32)]
 
 
 _lib = None
@@ -94,6 +110,17 @@ def load_library(path: str = LIB_PATH):
     lib.deer_debug_gemm_tiled.argtypes = [C.c_void_p, C.c_int]
     lib.deer_debug_gemm_block.argtypes = [C.c_void_p, C.c_int, C.c_int, C.c_int]
     lib.deer_debug_profile_read.argtypes = [C.c_void_p, C.c_int, C.POINTER(C.c_double), C.POINTER(C.c_int64), C.POINTER(C.c_double)]
+    lib.deer_kv8_last_error.restype = C.c_char_p
+    lib.deer_kv8_last_error.argtypes = [C.c_void_p]
+    lib.deer_kv8_query_sizes.argtypes = [C.POINTER(Kv8Params), C.POINTER(Kv8Sizes)]
+    lib.deer_kv8_init.argtypes = [C.POINTER(Kv8Params), C.c_void_p, C.c_void_p, C.POINTER(Kv8Sizes), C.POINTER(C.c_void_p)]
+    lib.deer_kv8_reserve.argtypes = [C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32]
+    lib.deer_kv8_append.argtypes = [C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_int, C.c_int64, C.c_int64, C.c_int32]
+    lib.deer_kv8_attend.argtypes = [C.c_void_p, C.c_int32, C.c_void_p, C.c_int, C.c_int64, C.c_void_p, C.c_float, C.c_void_p, C.c_int64, C.c_int32]
+    lib.deer_kv8_read.argtypes = [C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_int]
+    lib.deer_kv8_status.argtypes = [C.c_void_p, C.POINTER(C.c_int32), C.POINTER(C.c_int32)]
+    lib.deer_kv8_get_tables.argtypes = [C.c_void_p, C.POINTER(Kv8Tables)]
+    lib.deer_kv8_destroy.argtypes = [C.c_void_p]
     _lib = lib
     return lib
 
@@ -323,3 +350,150 @@ class DeerEngine:
 
     def synchronize(self):
         self.torch.cuda.current_stream(self.device).synchronize()
+
+
+def kv8_params(n_layers, n_q_heads, n_kv_heads, head_dim, max_batch, max_seq, n_pages=0, max_rows=1, device=0, stream=0) -> Kv8Params:
+    return Kv8Params(C.sizeof(Kv8Params), 1, n_layers, n_q_heads, n_kv_heads, head_dim, max_batch, max_seq, n_pages, max_rows, device, stream)
+
+
+class Kv8Cache:
+    """A paged 8-bit KV cache (see deer_kv8_* in include/deer.h) over torch tensors.  Method names follow the C ABI.
+
+    Work is enqueued on the stream that is current when the cache is made; a call from another current stream waits for
+    that stream first, and that stream then for the call."""
+
+    def __init__(self, n_layers, n_q_heads, n_kv_heads, head_dim, max_batch, max_seq, n_pages=0, max_rows=None, device=0):
+        import torch
+        self.torch = torch
+        self.lib = load_library()
+        self.ctx = None
+        if not torch.cuda.is_available():
+            raise RuntimeError("Kv8Cache needs a GPU: libdeer has no CPU path")
+        self.device = torch.device("cuda", device)
+        self.stream = torch.cuda.current_stream(self.device)
+        self.n_layers, self.n_q_heads, self.n_kv_heads, self.head_dim = n_layers, n_q_heads, n_kv_heads, head_dim
+        self.max_batch, self.max_seq = max_batch, max_seq
+        self.max_rows = 64 * max_batch if max_rows is None else max_rows
+        self.params = kv8_params(n_layers, n_q_heads, n_kv_heads, head_dim, max_batch, max_seq, n_pages, self.max_rows, device,
+                                 self.stream.cuda_stream)
+        self.sizes = Kv8Sizes()
+        self._check(self.lib.deer_kv8_query_sizes(C.byref(self.params), C.byref(self.sizes)))
+        self._cache = torch.empty(self.sizes.cache, dtype=torch.uint8, device=self.device)
+        self._workspace = torch.empty(self.sizes.workspace, dtype=torch.uint8, device=self.device)
+        ctx = C.c_void_p()
+        self._check(self.lib.deer_kv8_init(C.byref(self.params), self._cache.data_ptr(), self._workspace.data_ptr(), C.byref(self.sizes),
+                                           C.byref(ctx)))
+        self.ctx = ctx
+        t = Kv8Tables()
+        self._check(self.lib.deer_kv8_get_tables(self.ctx, C.byref(t)))
+        self.block_table = self._view(self._cache, t.block_table, max_batch * t.max_blocks).view(max_batch, t.max_blocks)
+        self.lengths = self._view(self._cache, t.lengths, max_batch)
+        self.pages_held = self._view(self._cache, t.pages_held, max_batch)
+        self.row_offsets = self._view(self._workspace, t.row_offsets, max_batch + 1)
+        self.slots = self._view(self._workspace, t.slots, self.max_rows)
+        self.row_seq = self._view(self._workspace, t.row_seq, self.max_rows)
+        self.row_pos = self._view(self._workspace, t.row_pos, self.max_rows)
+        self.rows = 0
+
+    # -- helpers ---------------------------------------------------------------------------------
+    def _check(self, rc):
+        if rc:
+            raise DeerError(rc, self.lib.deer_kv8_last_error(self.ctx).decode())
+
+    def _view(self, buf, ptr, n):
+        off = ptr - buf.data_ptr()
+        return buf[off:off + 4 * n].view(self.torch.int32)
+
+    def _call(self, fn, tensors, *args):
+        """One call on the cache's stream, ordered with the current one."""
+        if self.ctx is None:
+            raise RuntimeError("the cache is closed")
+        cur = self.torch.cuda.current_stream(self.device)
+        other = cur.cuda_stream != self.stream.cuda_stream
+        if other:
+            self.stream.wait_stream(cur)
+            for t in tensors:
+                t.record_stream(self.stream)
+        self._check(fn(self.ctx, *args))
+        if other:
+            cur.wait_stream(self.stream)
+
+    def _ints(self, x, n, what):
+        if x.device != self.device or x.dtype != self.torch.int32 or not x.is_contiguous() or x.numel() != n:
+            raise ValueError(f"{what} must be {n} contiguous int32 on {self.device}")
+        return x
+
+    def _rows_of(self, x, heads, what):
+        """The row stride of x [rows][heads][head_dim]; heads and channels are dense."""
+        if x.device != self.device or x.dim() != 3 or tuple(x.shape) != (self.rows, heads, self.head_dim):
+            raise ValueError(f"{what} must be [{self.rows}][{heads}][{self.head_dim}] on {self.device}")
+        if x.dtype not in (self.torch.float32, self.torch.bfloat16):
+            raise TypeError(f"{what} must be float32 or bfloat16")
+        width = heads * self.head_dim
+        if self.rows and (x.stride(2) != 1 or (heads > 1 and x.stride(1) != self.head_dim)):
+            raise ValueError(f"{what}: a row's heads must be dense")
+        return x.stride(0) if self.rows > 1 else width
+
+    def _dtype(self, x):
+        return DEER_F32 if x.dtype == self.torch.float32 else DEER_BF16
+
+    def close(self):
+        if getattr(self, "ctx", None):
+            self.lib.deer_kv8_destroy(self.ctx)
+            self.ctx = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    # -- a pass ----------------------------------------------------------------------------------
+    def reserve(self, start, new, rows, max_new, max_len):
+        """start, new: int32 device tensors, an entry per sequence of the batch.  Returns the rows' slots (a view)."""
+        n = start.numel()
+        self._ints(start, n, "start")
+        self._ints(new, n, "new")
+        self._call(self.lib.deer_kv8_reserve, (start, new), n, start.data_ptr(), new.data_ptr(), rows, max_new, max_len)
+        self.rows = rows
+        return self.slots[:rows]
+
+    def append(self, layer, k, v):
+        """k, v: [rows][n_kv_heads][head_dim], float32 or bfloat16; rows may be strided."""
+        ks, vs = self._rows_of(k, self.n_kv_heads, "k"), self._rows_of(v, self.n_kv_heads, "v")
+        if k.dtype != v.dtype:
+            raise TypeError("k and v must have the same dtype")
+        self._call(self.lib.deer_kv8_append, (k, v), layer, k.data_ptr(), v.data_ptr(), self._dtype(k), ks, vs, self.rows)
+
+    def attend(self, layer, q, limits=None, out=None, scale=0.0):
+        """q: [rows][n_q_heads][head_dim], float32 or bfloat16; rows may be strided.  Returns the result, of q's dtype."""
+        qs = self._rows_of(q, self.n_q_heads, "q")
+        if limits is not None:
+            self._ints(limits, self.rows, "limits")
+        if out is None:
+            out = self.torch.empty((self.rows, self.n_q_heads, self.head_dim), dtype=q.dtype, device=self.device)
+        os_ = self._rows_of(out, self.n_q_heads, "out")
+        if out.dtype != q.dtype:
+            raise TypeError("out must have q's dtype")
+        self._call(self.lib.deer_kv8_attend, (q, out) + (() if limits is None else (limits,)), layer, q.data_ptr(), self._dtype(q), qs,
+                   None if limits is None else limits.data_ptr(), scale, out.data_ptr(), os_, self.rows)
+        return out
+
+    def read(self, layer, seq, pos, dtype=None):
+        """(k, v) [n][n_kv_heads][head_dim] of the tokens (seq[i], pos[i]) as the cache holds them, bfloat16 or float32."""
+        n = seq.numel()
+        self._ints(seq, n, "seq")
+        self._ints(pos, n, "pos")
+        dtype = dtype or self.torch.bfloat16
+        if dtype not in (self.torch.float32, self.torch.bfloat16):
+            raise TypeError("dtype must be float32 or bfloat16")
+        k = self.torch.empty((n, self.n_kv_heads, self.head_dim), dtype=dtype, device=self.device)
+        v = self.torch.empty_like(k)
+        self._call(self.lib.deer_kv8_read, (seq, pos, k, v), layer, seq.data_ptr(), pos.data_ptr(), n, k.data_ptr(), v.data_ptr(), self._dtype(k))
+        return k, v
+
+    def status(self):
+        """(free pages, sequences that the last reserve refused)"""
+        free, refused = C.c_int32(), C.c_int32()
+        self._call(lambda *a: self.lib.deer_kv8_status(*a), (), C.byref(free), C.byref(refused))
+        return free.value, refused.value

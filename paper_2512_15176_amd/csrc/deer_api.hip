@@ -3,6 +3,7 @@
 #include "deer_kernels.hpp"
 #include "deer_block.hpp"
 #include "deer_stream.hpp"
+#include "deer_kv8_host.hpp"
 
 #include <algorithm>
 #include <cmath>
@@ -104,6 +105,13 @@ struct Work : PassBufs {   // carved from the workspace
 enum State { ST_INIT = 0, ST_PREFILLED, ST_DRAFTED, ST_VERIFIED };
 
 }  // namespace
+
+struct deer_kv8 {
+    Kv8Cache c;
+    int device = 0;
+    hipStream_t stream = nullptr;
+    std::string err;
+};
 
 struct deer_ctx {
     deer_init_params p{};
@@ -1535,5 +1543,193 @@ int deer_get_kv_layout(const deer_ctx *c, int model, deer_kv_layout *out) {
     out->max_seq = c->p.max_seq; out->head_dim = m.c.head_dim;
     return DEER_OK;
 }
+
+// ---------------------------------------------------------------------------------------------
+// paged 8-bit KV cache
+// ---------------------------------------------------------------------------------------------
+}  // extern "C"
+
+namespace {
+
+int fail8(deer_kv8 *c, int code, const char *what, const char *detail = "") {
+    std::string &s = c ? c->err : g_init_error;
+    s = what;
+    if (*detail) (s += ": ") += detail;
+    return code;
+}
+
+// The handle's device is current while a call launches; the caller's is put back.
+struct DeviceScope {
+    int old = -1;
+    hipError_t err = hipSuccess;
+    explicit DeviceScope(int device) {
+        err = hipGetDevice(&old);
+        if (err == hipSuccess && old != device) err = hipSetDevice(device); else old = -1;
+    }
+    ~DeviceScope() { if (old >= 0 && err == hipSuccess) (void)hipSetDevice(old); }
+};
+
+#define KV8CHK(c, expr)                                                                        \
+    do {                                                                                       \
+        hipError_t e_ = (expr);                                                                \
+        if (e_ != hipSuccess) return fail8((c), DEER_EHIP, #expr, hipGetErrorString(e_));      \
+    } while (0)
+
+Kv8Shape kv8_shape(const deer_kv8_params *p) {
+    Kv8Shape s{p->n_layers, p->n_q_heads, p->n_kv_heads, p->head_dim, p->max_batch, p->max_seq, p->n_pages, p->max_rows};
+    if (s.n_pages == 0 && s.max_batch > 0 && s.max_batch <= KV8_MAX_BATCH && s.max_seq > 0 && s.max_seq <= 1 << 20) s.n_pages = s.max_batch * (s.max_seq / KV8_PAGE);
+    return s;
+}
+
+// a row stride in elements that keeps 16-byte loads aligned, over rows of at least `width`
+bool kv8_stride_ok(int64_t stride, int64_t width, int dtype) { return stride >= width && stride % (dtype == DEER_F32 ? 4 : 8) == 0 && stride < (int64_t)1 << 32; }
+bool kv8_dtype_ok(int dtype) { return dtype == DEER_F32 || dtype == DEER_BF16; }
+bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
+bool aligned4(const void *p) { return ((uintptr_t)p & 3) == 0; }
+
+}  // namespace
+
+extern "C" {
+
+int deer_kv8_query_sizes(const deer_kv8_params *p, deer_kv8_sizes *out) {
+    if (!p || !out) return fail8(nullptr, DEER_EINVAL, "null argument");
+    if (p->struct_size != sizeof(deer_kv8_params) || p->abi_version != DEER_ABI_VERSION) return fail8(nullptr, DEER_EVERSION, "struct_size/abi_version mismatch");
+    const Kv8Shape s = kv8_shape(p);
+    if (const char *e = check_kv8(s)) return fail8(nullptr, DEER_EINVAL, e);
+    Kv8Cache c;
+    plan_kv8(c, s, nullptr, nullptr);
+    out->cache = c.cache_bytes;
+    out->workspace = c.work_bytes;
+    return DEER_OK;
+}
+
+int deer_kv8_init(const deer_kv8_params *p, void *cache_dev, void *workspace_dev, const deer_kv8_sizes *buf_sizes, deer_kv8 **out) {
+    if (out) *out = nullptr;
+    if (!out || !buf_sizes) return fail8(nullptr, DEER_EINVAL, "null argument");
+    deer_kv8_sizes need;
+    if (int rc = deer_kv8_query_sizes(p, &need)) return rc;
+    if (!cache_dev || !workspace_dev || ((uintptr_t)cache_dev & 255) || ((uintptr_t)workspace_dev & 255)) return fail8(nullptr, DEER_EINVAL, "null or unaligned device buffer");
+    if (buf_sizes->cache < need.cache || buf_sizes->workspace < need.workspace) return fail8(nullptr, DEER_ECAPACITY, "cache or workspace buffer too small");
+    deer_kv8 *c = new (std::nothrow) deer_kv8();
+    if (!c) return fail8(nullptr, DEER_EINVAL, "out of host memory");
+    c->device = p->device;
+    c->stream = (hipStream_t)p->hip_stream;
+    plan_kv8(c->c, kv8_shape(p), (char *)cache_dev, (char *)workspace_dev);
+    DeviceScope dev(c->device);
+    hipError_t e = dev.err;
+    if (e == hipSuccess) e = kv8_clear(c->c, c->stream);
+    if (e == hipSuccess) e = hipStreamSynchronize(c->stream);
+    if (e != hipSuccess) { delete c; return fail8(nullptr, DEER_EHIP, "clearing the cache", hipGetErrorString(e)); }
+    *out = c;
+    return DEER_OK;
+}
+
+int deer_kv8_reserve(deer_kv8 *c, int32_t batch, const int32_t *start_dev, const int32_t *new_dev, int32_t rows, int32_t max_new, int32_t max_len) {
+    if (!c) return DEER_EINVAL;
+    if (!start_dev || !new_dev || !aligned4(start_dev) || !aligned4(new_dev)) return fail8(c, DEER_EINVAL, "null or unaligned pointer");
+    if (const char *e = check_kv8_pass(c->c, batch, rows, max_new, max_len)) return fail8(c, DEER_EINVAL, e);
+    DeviceScope dev(c->device);
+    KV8CHK(c, dev.err);
+    KV8CHK(c, kv8_reserve(c->c, c->stream, start_dev, 0, new_dev, 0, batch, rows, max_new, max_len));
+    return DEER_OK;
+}
+
+int deer_kv8_append(deer_kv8 *c, int32_t layer, const void *k_dev, const void *v_dev, int dtype, int64_t k_stride, int64_t v_stride, int32_t rows) {
+    if (!c) return DEER_EINVAL;
+    const Kv8Shape &p = c->c.p;
+    if (c->c.batch == 0) return fail8(c, DEER_ESTATE, "append needs the tables of a pass (deer_kv8_reserve)");
+    if (layer < 0 || layer >= p.n_layers) return fail8(c, DEER_EINVAL, "layer out of range");
+    if (rows != c->c.rows) return fail8(c, DEER_EINVAL, "rows must be those of the pass");
+    if (rows == 0) return DEER_OK;
+    const int64_t width = (int64_t)p.n_kv_heads * p.head_dim;
+    if (!k_dev || !v_dev || !aligned16(k_dev) || !aligned16(v_dev)) return fail8(c, DEER_EINVAL, "null or unaligned pointer");
+    if (!kv8_dtype_ok(dtype)) return fail8(c, DEER_EINVAL, "dtype must be DEER_F32 or DEER_BF16");
+    if (!kv8_stride_ok(k_stride, width, dtype) || !kv8_stride_ok(v_stride, width, dtype)) return fail8(c, DEER_EINVAL, "row strides must cover the heads and keep 16-byte alignment");
+    DeviceScope dev(c->device);
+    KV8CHK(c, dev.err);
+    if (dtype == DEER_F32) KV8CHK(c, kv8_write(c->c, c->stream, layer, (const float *)k_dev, (const float *)v_dev, (size_t)k_stride, (size_t)v_stride));
+    else KV8CHK(c, kv8_write(c->c, c->stream, layer, (const uint16_t *)k_dev, (const uint16_t *)v_dev, (size_t)k_stride, (size_t)v_stride));
+    KV8CHK(c, kv8_settle(c->c, c->stream, layer));
+    return DEER_OK;
+}
+
+int deer_kv8_attend(deer_kv8 *c, int32_t layer, const void *q_dev, int dtype, int64_t q_stride, const int32_t *limits_dev, float scale, void *out_dev,
+                    int64_t out_stride, int32_t rows) {
+    if (!c) return DEER_EINVAL;
+    const Kv8Shape &p = c->c.p;
+    if (c->c.batch == 0) return fail8(c, DEER_ESTATE, "attend needs the tables of a pass (deer_kv8_reserve)");
+    if (layer < 0 || layer >= p.n_layers) return fail8(c, DEER_EINVAL, "layer out of range");
+    if (rows != c->c.rows) return fail8(c, DEER_EINVAL, "rows must be those of the pass");
+    if (!(scale >= 0.f && scale < 1e30f)) return fail8(c, DEER_EINVAL, "scale must be positive, or 0 for 1 / sqrt(head_dim)");
+    if (rows == 0) return DEER_OK;
+    const int64_t width = (int64_t)p.n_q_heads * p.head_dim;
+    if (!q_dev || !out_dev || !aligned16(q_dev) || !aligned16(out_dev) || !aligned4(limits_dev)) return fail8(c, DEER_EINVAL, "null or unaligned pointer");
+    if (!kv8_dtype_ok(dtype)) return fail8(c, DEER_EINVAL, "dtype must be DEER_F32 or DEER_BF16");
+    if (!kv8_stride_ok(q_stride, width, dtype) || !kv8_stride_ok(out_stride, width, dtype)) return fail8(c, DEER_EINVAL, "row strides must cover the heads and keep 16-byte alignment");
+    DeviceScope dev(c->device);
+    KV8CHK(c, dev.err);
+    Kv8Attn a{};
+    a.limits = limits_dev; a.q = q_dev; a.out = out_dev; a.q_stride = q_stride; a.out_stride = out_stride;
+    const double sc = scale > 0.f ? (double)scale : 1.0 / std::sqrt((double)p.head_dim);
+    if (dtype == DEER_F32) KV8CHK(c, kv8_attend<KV8_F32>(c->c, c->stream, layer, a, sc));
+    else KV8CHK(c, kv8_attend<KV8_BF16>(c->c, c->stream, layer, a, sc));
+    return DEER_OK;
+}
+
+int deer_kv8_read(deer_kv8 *c, int32_t layer, const int32_t *seq_dev, const int32_t *pos_dev, int32_t n, void *k_dev, void *v_dev, int dtype) {
+    if (!c) return DEER_EINVAL;
+    const Kv8Shape &p = c->c.p;
+    if (layer < 0 || layer >= p.n_layers) return fail8(c, DEER_EINVAL, "layer out of range");
+    if (n < 0) return fail8(c, DEER_EINVAL, "n must not be negative");
+    if (!kv8_dtype_ok(dtype)) return fail8(c, DEER_EINVAL, "dtype must be DEER_F32 or DEER_BF16");
+    if (n == 0) return DEER_OK;
+    if (!seq_dev || !pos_dev || !k_dev || !v_dev || !aligned4(seq_dev) || !aligned4(pos_dev) || !aligned16(k_dev) || !aligned16(v_dev))
+        return fail8(c, DEER_EINVAL, "null or unaligned pointer");
+    const size_t items = (size_t)n * p.n_kv_heads * (p.head_dim / 8);
+    if ((items + 255) / 256 > 0x7fffffffu) return fail8(c, DEER_EINVAL, "too many rows for one call");
+    DeviceScope dev(c->device);
+    KV8CHK(c, dev.err);
+    const dim3 grid((unsigned)((items + 255) / 256));
+    const Kv8Hot ring = c->c.ring_view(layer);
+    if (dtype == DEER_F32)
+        hipLaunchKernelGGL(k_kv8_read<float>, grid, dim3(256), 0, c->stream, c->c.st, seq_dev, pos_dev, n, ring, c->c.layer_pages(layer), c->c.layer_scales(layer),
+                           p.n_kv_heads, p.head_dim, (float *)k_dev, (float *)v_dev);
+    else
+        hipLaunchKernelGGL(k_kv8_read<uint16_t>, grid, dim3(256), 0, c->stream, c->c.st, seq_dev, pos_dev, n, ring, c->c.layer_pages(layer), c->c.layer_scales(layer),
+                           p.n_kv_heads, p.head_dim, (uint16_t *)k_dev, (uint16_t *)v_dev);
+    KV8CHK(c, hipGetLastError());
+    return DEER_OK;
+}
+
+int deer_kv8_status(deer_kv8 *c, int32_t *free_pages, int32_t *refused) {
+    if (!c) return DEER_EINVAL;
+    if (!free_pages || !refused) return fail8(c, DEER_EINVAL, "null pointer");
+    int st[2] = {0, 0};
+    DeviceScope dev(c->device);
+    KV8CHK(c, dev.err);
+    KV8CHK(c, hipMemcpyAsync(st, c->c.st.stat, sizeof st, hipMemcpyDeviceToHost, c->stream));
+    KV8CHK(c, hipStreamSynchronize(c->stream));
+    *free_pages = st[0]; *refused = st[1];
+    return DEER_OK;
+}
+
+int deer_kv8_get_tables(const deer_kv8 *c, deer_kv8_tables *out) {
+    if (!c || !out) return DEER_EINVAL;
+    const Kv8State &s = c->c.st;
+    *out = deer_kv8_tables{s.table, s.len, s.held, s.cu, s.slot, s.row_seq, s.row_pos, s.max_blocks};
+    return DEER_OK;
+}
+
+int deer_kv8_destroy(deer_kv8 *c) {
+    if (!c) return DEER_EINVAL;
+    {
+        DeviceScope dev(c->device);
+        (void)hipStreamSynchronize(c->stream);
+    }
+    delete c;
+    return DEER_OK;
+}
+
+const char *deer_kv8_last_error(const deer_kv8 *c) { return c ? c->err.c_str() : g_init_error.c_str(); }
 
 }  // extern "C"

@@ -1,0 +1,163 @@
+// Host side of the paged 8-bit KV cache: where its parts lie, launch shapes, argument checks.  A deer_kv8 handle has one of these,
+// and so has a context whose target cache is kept in 8 bits.
+#pragma once
+#include "deer_kv8.hpp"
+
+#include <algorithm>
+#include <cmath>
+
+namespace deer {
+
+// Tiles of 32 packed rows whose un-normalised results of a key range the workspace holds: what 512 workgroups of four tiles leave, twice.
+constexpr int KV8_PART_TILES = 4096;
+constexpr int KV8_WGS = 512;          // workgroups that fill the chip: two per compute unit
+
+struct Kv8Shape { int n_layers, n_q_heads, n_kv_heads, head_dim, max_batch, max_seq, n_pages, max_rows; };
+
+struct Kv8Cache {
+    Kv8Shape p{};
+    Kv8State st{};
+    uint8_t *pages = nullptr;
+    float *scales = nullptr, *part = nullptr;
+    uint16_t *ring = nullptr, *scratch = nullptr;
+    size_t scratch_slots = 0, cache_bytes = 0, work_bytes = 0;
+    // the pass
+    int batch = 0, rows = 0, max_new = 0, max_len = 0;
+    bool long_pass = false;      // rows in the scratch
+
+    size_t page_bytes() const { return (size_t)p.n_kv_heads * 2 * KV8_PAGE * p.head_dim; }
+    size_t ring_layer() const { return (size_t)p.max_batch * p.n_kv_heads * KV8_SLOTS * p.head_dim; }   // elements of K, and of V
+    Kv8Hot ring_view(int layer) const {
+        uint16_t *k = ring + 2 * (size_t)layer * ring_layer();
+        return Kv8Hot{k, k + ring_layer(), (size_t)p.n_kv_heads * KV8_SLOTS * p.head_dim, (size_t)KV8_SLOTS * p.head_dim, KV8_RING - 1};
+    }
+    // where the pass's rows of a layer are (the scratch serves one layer after the other)
+    Kv8Hot hot_view(int layer) const {
+        if (!long_pass) return ring_view(layer);
+        return Kv8Hot{scratch, scratch + scratch_slots * p.n_kv_heads * p.head_dim, 0, scratch_slots * p.head_dim, -1};
+    }
+    uint8_t *layer_pages(int layer) const { return pages + (size_t)layer * p.n_pages * page_bytes(); }
+    float *layer_scales(int layer) const { return scales + (size_t)layer * p.n_pages * p.n_kv_heads * 2; }
+};
+
+inline const char *check_kv8(const Kv8Shape &p) {
+    if (p.n_layers < 1 || p.n_layers > 1024) return "n_layers must be in 1..1024";
+    if (p.head_dim != 32 && p.head_dim != 64 && p.head_dim != 128) return "head_dim must be 32, 64 or 128";
+    if (p.n_kv_heads < 1 || p.n_kv_heads > 1024 || p.n_q_heads < 1 || p.n_q_heads % p.n_kv_heads) return "n_q_heads must be a multiple of n_kv_heads";
+    if (p.n_q_heads / p.n_kv_heads > 64) return "more than 64 query heads per kv head";
+    if (p.max_batch < 1 || p.max_batch > KV8_MAX_BATCH) return "max_batch must be in 1..1024";
+    if (p.max_seq < KV8_PAGE || p.max_seq % KV8_PAGE || p.max_seq > 1 << 20) return "max_seq must be a multiple of 64, at most 2^20";
+    if (p.n_pages < 1 || p.n_pages > 1 << 24) return "n_pages must be in 1..2^24";
+    if (p.max_rows < 1 || p.max_rows > 1 << 20) return "max_rows must be in 1..2^20";
+    return nullptr;
+}
+
+// Carves the cache (pages, scales, ring, tables) and the workspace (the pass's arrays, scratch, partial results); with null
+// bases only the sizes.
+inline void plan_kv8(Kv8Cache &c, const Kv8Shape &p, char *cache, char *work) {
+    c.p = p;
+    size_t off = 0;
+    char *base = cache;
+    auto take = [&](size_t bytes) { size_t o = off; off = (off + bytes + 255) / 256 * 256; return base ? base + o : nullptr; };
+    c.pages = (uint8_t *)take((size_t)p.n_layers * p.n_pages * c.page_bytes());
+    c.scales = (float *)take((size_t)p.n_layers * p.n_pages * p.n_kv_heads * 2 * 4);
+    c.ring = (uint16_t *)take((size_t)p.n_layers * 2 * c.ring_layer() * 2);
+    Kv8State &s = c.st;
+    s.max_blocks = p.max_seq / KV8_PAGE; s.max_batch = p.max_batch; s.n_pages = p.n_pages; s.max_rows = p.max_rows;
+    s.table = (int *)take((size_t)p.max_batch * s.max_blocks * 4);
+    s.len = (int *)take(p.max_batch * 4); s.held = (int *)take(p.max_batch * 4); s.hot = (int *)take(p.max_batch * 4); s.base = (int *)take(p.max_batch * 4);
+    s.free = (int *)take((size_t)p.n_pages * 4);
+    s.stat = (int *)take(8 * 4);
+    c.cache_bytes = off;
+    off = 0; base = work;
+    s.start = (int *)take(p.max_batch * 4); s.count = (int *)take(p.max_batch * 4); s.hotbase = (int *)take(p.max_batch * 4); s.carry = (int *)take(p.max_batch * 4);
+    s.cu = (int *)take((p.max_batch + 1) * 4);
+    s.slot = (int *)take((size_t)p.max_rows * 4); s.row_seq = (int *)take((size_t)p.max_rows * 4); s.row_pos = (int *)take((size_t)p.max_rows * 4);
+    // a sequence's rows of a long pass touch whole pages: up to 127 slots more than rows
+    c.scratch_slots = p.max_rows > KV8_PAGE ? ((size_t)p.max_rows + (size_t)std::min(p.max_batch, p.max_rows) * 127 + 63) / 64 * 64 : 0;
+    c.scratch = (uint16_t *)take(2 * c.scratch_slots * p.n_kv_heads * p.head_dim * 2);
+    c.part = (float *)take((size_t)KV8_PART_TILES * (32 * p.head_dim + 64) * 4);
+    c.work_bytes = off;
+}
+
+// everything finite, no tokens (masked keys are multiplied by zero weights)
+inline hipError_t kv8_clear(Kv8Cache &c, hipStream_t s) {
+    hipError_t e = hipMemsetAsync(c.pages, 0, (char *)c.st.table - (char *)c.pages, s);
+    if (e == hipSuccess && c.scratch_slots) e = hipMemsetAsync(c.scratch, 0, (char *)c.part - (char *)c.scratch, s);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(k_kv8_init, dim3(256), dim3(256), 0, s, c.st);
+    c.batch = c.rows = 0;
+    return hipGetLastError();
+}
+
+inline const char *check_kv8_pass(const Kv8Cache &c, int batch, int rows, int max_new, int max_len) {
+    if (batch < 1 || batch > c.p.max_batch) return "batch must be in 1..max_batch";
+    if (rows < 0 || rows > c.p.max_rows) return "rows must be in 0..max_rows";
+    if (max_new < 0 || max_new > c.p.max_seq) return "max_new must be in 0..max_seq";
+    if (max_len < 0 || max_len > c.p.max_seq) return "max_len must be in 0..max_seq";
+    if (((long long)max_new * (c.p.n_q_heads / c.p.n_kv_heads) + 31) / 32 > 65535) return "max_new is too large for one pass";
+    return nullptr;
+}
+
+inline hipError_t kv8_reserve(Kv8Cache &c, hipStream_t s, const int *start, int start_add, const int *count, int count_const, int batch, int rows,
+                              int max_new, int max_len) {
+    max_new = std::min(max_new, std::max(rows, 0));
+    c.batch = batch; c.rows = rows; c.max_new = max_new; c.max_len = max_len;
+    c.long_pass = max_new > KV8_PAGE;
+    const int wgs = std::max(1, std::min(64, (rows + 4095) / 4096));
+    hipLaunchKernelGGL(k_kv8_reserve, dim3(wgs), dim3(1024), 0, s, c.st, start, start_add, count, count_const, batch, rows, max_new, max_len, c.long_pass ? 1 : 0);
+    return hipGetLastError();
+}
+
+template <int HD>
+hipError_t kv8_settle_hd(Kv8Cache &c, hipStream_t s, int layer) {
+    const Kv8Hot ring = c.long_pass ? c.ring_view(layer) : Kv8Hot{};
+    hipLaunchKernelGGL(k_kv8_settle<HD>, dim3((c.max_new + KV8_PAGE - 2) / KV8_PAGE + 1, c.p.n_kv_heads, c.batch), dim3(256), 0, s, c.st, c.hot_view(layer), ring,
+                       c.layer_pages(layer), c.layer_scales(layer), c.p.n_kv_heads);
+    return hipGetLastError();
+}
+// the pass's rows of the layer are in the hot pages: complete pages go to the pool
+inline hipError_t kv8_settle(Kv8Cache &c, hipStream_t s, int layer) {
+    if (c.rows == 0 || c.max_new == 0) return hipSuccess;
+    return c.p.head_dim == 128 ? kv8_settle_hd<128>(c, s, layer) : c.p.head_dim == 64 ? kv8_settle_hd<64>(c, s, layer) : kv8_settle_hd<32>(c, s, layer);
+}
+
+template <typename T>
+hipError_t kv8_write(Kv8Cache &c, hipStream_t s, int layer, const T *k, const T *v, size_t k_stride, size_t v_stride) {
+    const Kv8Shape &p = c.p;
+    if (c.rows == 0) return hipSuccess;
+    const size_t items = (size_t)c.rows * p.n_kv_heads * (p.head_dim / 8);
+    const unsigned row_wgs = (unsigned)((items + 255) / 256);
+    hipLaunchKernelGGL(k_kv8_write<T>, dim3(row_wgs + c.batch * p.n_kv_heads), dim3(256), 0, s, c.st, k, v, k_stride, v_stride, c.hot_view(layer), c.ring_view(layer),
+                       c.rows, (int)row_wgs, p.n_kv_heads, p.head_dim);
+    return hipGetLastError();
+}
+
+template <int HD, int SRC>
+hipError_t kv8_attend_src(Kv8Cache &c, hipStream_t s, Kv8Attn &a) {
+    const int B = c.batch, packed = c.max_new * a.G, pages = (c.max_len + KV8_PAGE - 1) / KV8_PAGE;
+    a.rts = (packed + 31) / 32;
+    const bool few = packed <= 32;
+    const int ty = few ? a.rts : (a.rts + 3) / 4;
+    const long long items = (long long)B * ty * a.Hkv, tiles = (long long)B * a.rts * a.Hkv;
+    // key ranges: as many as fill the chip, each with work for all of its waves
+    a.NS = (int)std::max<long long>(1, std::min<long long>({KV8_WGS / std::max<long long>(items, 1), KV8_PART_TILES / tiles, 64, std::max(1, pages / 4)}));
+    const dim3 grid(a.Hkv * a.NS, ty, B);
+    if (few) hipLaunchKernelGGL((k_kv8_attn_few<HD, SRC>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((k_kv8_attn_many<HD, SRC>), grid, dim3(256), 0, s, a);
+    if (hipError_t e = hipGetLastError()) return e;
+    if (a.NS > 1) hipLaunchKernelGGL((k_kv8_merge<HD, SRC>), dim3(a.Hkv, a.rts, B), dim3(64), 0, s, a);
+    return hipGetLastError();
+}
+// a: what the caller knows (limits, q, out or fragments)
+template <int SRC>
+hipError_t kv8_attend(Kv8Cache &c, hipStream_t s, int layer, Kv8Attn a, double scale) {
+    if (c.rows == 0 || c.max_new == 0) return hipSuccess;
+    a.s = c.st; a.hot = c.hot_view(layer); a.pages = c.layer_pages(layer); a.scales = c.layer_scales(layer);
+    a.part = c.part; a.Hq = c.p.n_q_heads; a.Hkv = c.p.n_kv_heads; a.G = a.Hq / a.Hkv; a.rows = c.rows;
+    a.scale_log2e = (float)(scale * 1.4426950408889634);
+    a.m_init = -3e38f / std::max(1.f, a.scale_log2e);     // times scale_log2e it stays finite
+    return c.p.head_dim == 128 ? kv8_attend_src<128, SRC>(c, s, a) : c.p.head_dim == 64 ? kv8_attend_src<64, SRC>(c, s, a) : kv8_attend_src<32, SRC>(c, s, a);
+}
+
+}  // namespace deer
