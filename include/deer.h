@@ -54,6 +54,7 @@ typedef enum {
 
 enum { DEER_TARGET = 0, DEER_DRAFTER = 1 };
 enum { DEER_F32 = 0, DEER_BF16 = 1 };
+enum { DEER_KV_BF16 = 0, DEER_KV_E4M3 = 1 };   /* how the target's cache is kept (deer_init_params) */
 
 /* Tensor ids for deer_load_tensor.  Every projection is given in [in][out] row-major order
  * (y = x W); the embedding table is [vocab][d_model]. */
@@ -84,6 +85,14 @@ typedef struct {
     int32_t keep_logits;    /* 1: materialise [B][k][vocab] fp32 logits at T = 0 too (parity)     */
     int32_t device;         /* HIP device ordinal                                                 */
     void *hip_stream;       /* hipStream_t, default priority; NULL = the default stream          */
+    /* From here on optional: a struct_size that ends before them (offsetof target_kv_format) takes them as 0. */
+    int32_t target_kv_format; /* DEER_KV_E4M3: the target's cache in pages of 8 bits (see the paged 8-bit cache below; the drafter's stays
+                               * bf16).  Then max_seq <= 2^20, kv[DEER_TARGET] holds the paged cache, deer_get_kv_layout refuses the
+                               * target, deer_debug_load_kv takes the target's slots from a multiple of 64 or the end on (what lies
+                               * behind them is dropped), and deer_set_prefilled needs the first lens - 1 of a sequence's target
+                               * slots to have been loaded or prefilled, the last page of them in the last call or pass       */
+    int32_t target_kv_pages;  /* its pages of 64 tokens, shared by all sequences; 0: max_batch * max_seq / 64.  DEER_ECAPACITY where
+                               * a prompt, or a block behind a draft, does not fit the pages                                  */
 } deer_init_params;
 
 /* Bytes the caller must provide.  All buffers 256-byte aligned. */

@@ -12,6 +12,7 @@ LIB_PATH = os.path.join(PKG_DIR, "libdeer.so")
 
 DEER_TARGET, DEER_DRAFTER = 0, 1
 DEER_F32, DEER_BF16 = 0, 1
+DEER_KV_BF16, DEER_KV_E4M3 = 0, 1
 TENSOR_IDS = {"embed": 1, "lm_head": 2, "wq": 3, "wk": 4, "wv": 5, "wo": 6, "wg": 7, "wu": 8, "wd": 9, "router": 10}
 STATUS = {0: "DEER_OK", -1: "DEER_EINVAL", -2: "DEER_ESTATE", -3: "DEER_ECAPACITY", -4: "DEER_EHIP", -5: "DEER_EVERSION"}
 EXPORTS = ["deer_query_sizes", "deer_init_models", "deer_load_tensor", "deer_prefill", "deer_set_prefilled",
@@ -38,7 +39,8 @@ class ModelCfg(C.Structure):
 class InitParams(C.Structure):
     _fields_ = [("struct_size", C.c_uint32), ("abi_version", C.c_uint32), ("target", ModelCfg), ("drafter", ModelCfg),
                 ("max_batch", C.c_int32), ("max_seq", C.c_int32), ("max_k", C.c_int32), ("mask_token_id", C.c_int32),
-                ("eos_token_id", C.c_int32), ("keep_logits", C.c_int32), ("device", C.c_int32), ("hip_stream", C.c_void_p)]
+                ("eos_token_id", C.c_int32), ("keep_logits", C.c_int32), ("device", C.c_int32), ("hip_stream", C.c_void_p),
+                ("target_kv_format", C.c_int32), ("target_kv_pages", C.c_int32)]
 
 
 class Sizes(C.Structure):
@@ -132,9 +134,9 @@ def model_cfg(shape) -> ModelCfg:
 
 
 def init_params(target, drafter, max_batch, max_seq, max_k, mask_token_id, eos_token_id=-1, keep_logits=False,
-                device=0, stream=0) -> InitParams:
+                device=0, stream=0, kv_format=0, kv_pages=0) -> InitParams:
     return InitParams(C.sizeof(InitParams), 1, model_cfg(target), model_cfg(drafter), max_batch, max_seq, max_k,
-                      mask_token_id, eos_token_id, int(keep_logits), device, stream)
+                      mask_token_id, eos_token_id, int(keep_logits), device, stream, kv_format, kv_pages)
 
 
 def query_sizes(params: InitParams) -> Sizes:
@@ -150,7 +152,8 @@ class DeerEngine:
     """Owns the device buffers (torch tensors) and a libdeer context.  Method names follow the C ABI."""
 
     def __init__(self, target, drafter, max_batch, max_seq, max_k, mask_token_id, eos_token_id=-1, keep_logits=False,
-                 device=0):
+                 device=0, kv_format=DEER_KV_BF16, kv_pages=0):
+        """kv_format: DEER_KV_E4M3 keeps the target's cache in 8 bits, in kv_pages pages of 64 tokens (0: enough for all)."""
         import torch
         self.torch = torch
         self.lib = load_library()
@@ -162,7 +165,7 @@ class DeerEngine:
         self.max_batch, self.max_seq, self.max_k = max_batch, max_seq, max_k
         stream = torch.cuda.current_stream(self.device).cuda_stream
         self.params = init_params(target, drafter, max_batch, max_seq, max_k, mask_token_id, eos_token_id, keep_logits,
-                                  device, stream)
+                                  device, stream, kv_format, kv_pages)
         self.sizes = query_sizes(self.params)
         alloc = lambda n: torch.empty(max(int(n), 256), dtype=torch.uint8, device=self.device)
         self._weights = [alloc(self.sizes.weights[i]) for i in range(2)]

@@ -8,6 +8,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdarg>
+#include <cstddef>
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
@@ -125,6 +126,8 @@ struct deer_ctx {
     int cur_k = 0;
     float cur_T = 0.f;
     int max_tiles = 0;
+    bool kv8_on = false;             // the target's cache is kept in 8 bits
+    Kv8Cache kv8;
     int block_gemm = 128;            // deer_debug_gemm_tiled: 0 never blocked; 128 where it is estimated to be faster; less: from 8 row tiles on
     int force_nb = 0, force_ring = 0, force_S = 0;   // deer_debug_gemm_block; force_nb 0: off
     // deer_debug_gemm_stamps: which streaming-GEMM launch of which model's passes records its stamps
@@ -358,6 +361,23 @@ void plan_work(Work &w, const deer_init_params &p, char *base) {
     w.bytes = off;
 }
 
+bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
+
+Kv8Shape target_kv8_shape(const deer_init_params &p) {
+    const deer_model_cfg &t = p.target;
+    return Kv8Shape{t.n_layers, t.n_q_heads, t.n_kv_heads, t.head_dim, p.max_batch, p.max_seq, p.target_kv_pages ? p.target_kv_pages : p.max_batch * (p.max_seq / KV8_PAGE),
+                    32 * std::max(2 * p.max_batch, PREFILL_TILES)};
+}
+
+// The caller's parameters with the optional ones at the end filled in; false: another version.
+bool read_params(const deer_init_params *p, deer_init_params &out) {
+    out = deer_init_params{};
+    const size_t old = offsetof(deer_init_params, target_kv_format);
+    if ((p->struct_size != sizeof(deer_init_params) && p->struct_size != old) || p->abi_version != DEER_ABI_VERSION) return false;
+    memcpy(&out, p, p->struct_size);
+    return true;
+}
+
 const char *check_params(const deer_init_params *p) {
     if (!p) return "null params";
     if (p->max_batch < 1 || p->max_batch > 1024) return "max_batch out of range";
@@ -368,6 +388,11 @@ const char *check_params(const deer_init_params *p) {
     if (p->target.vocab != p->drafter.vocab) return "target and drafter must share the vocabulary";
     if (p->mask_token_id < 0 || p->mask_token_id >= p->drafter.vocab) return "mask_token_id outside the vocabulary";
     if (p->eos_token_id >= p->target.vocab) return "eos_token_id outside the vocabulary";
+    if (p->target_kv_format != DEER_KV_BF16 && p->target_kv_format != DEER_KV_E4M3) return "unknown target_kv_format";
+    if (p->target_kv_format == DEER_KV_E4M3) {
+        if (p->max_seq > 1 << 20) return "an 8-bit cache holds at most 2^20 tokens per sequence";
+        if (const char *e = check_kv8(target_kv8_shape(*p))) return e;
+    }
     return nullptr;
 }
 
@@ -706,6 +731,26 @@ int launch_attn(deer_ctx *c, ModelRT &m, int layer, int ntiles, int NS, int NS_h
     return DEER_OK;
 }
 
+// The same over the target's 8-bit cache; its rows' tables are in place (kv8_reserve).
+int launch_attn_kv8(deer_ctx *c, int layer, double kv_bytes, const PassRows &rows) {
+    Work &w = c->wk;
+    ProfScope ps(c, 1, kv_bytes);
+    Kv8Attn a{};
+    a.qhi = w.q_hi; a.qlo = w.q_lo; a.xhi = w.xb_hi; a.xlo = w.xb_lo;
+    a.q_row0 = rows.kind == ROWS_PREFILL ? c->kv8.ask_row0 : nullptr;
+    HIPCHK(c, kv8_attend<KV8_FRAG>(c->kv8, c->stream, layer, a, 1.0 / std::sqrt((double)c->m[DEER_TARGET].c.head_dim)));
+    return DEER_OK;
+}
+// A pass's rows go to the hot pages.
+void kv8_place(const deer_ctx *c, PassRows &pr) { pr.slot_base = c->kv8.st.hotbase; pr.slot_mask = c->kv8.long_pass ? -1 : KV8_RING - 1; }
+// Pages that the target's cache needs for n tokens of sequence b; false: the pool does not hold them.
+template <typename F>
+bool kv8_fits(const deer_ctx *c, int batch, F tokens) {
+    long long pages = 0;
+    for (int b = 0; b < batch; ++b) pages += (tokens(b) + KV8_PAGE - 1) / KV8_PAGE;
+    return pages <= c->kv8.p.n_pages;
+}
+
 // Up to how many pairs per expert, on average over all experts, a mixture's projections run in k_gemm_moe; with more of them
 // experts of more than 32 pairs, whose weights that kernel reads twice, become frequent.  128 experts of 2048 x 768, top 8,
 // microseconds k_gemm_moe / k_moe_block (gate/up: with k_moe_gather; medians of one sweep over three layers, rows spread evenly) at
@@ -737,6 +782,7 @@ int run_pass(deer_ctx *c, int model, int ntiles, int n_attn, int max_limit, cons
     // Not for a mixture: with it a row of the full-size mixture's test that lies between two experts went to the other one than
     // in the reference.  (Any order of sums can do that.  A mixture's key ranges per head and its launches in pieces have
     // changed theirs too, without such a row in the tests; what it would gain here has not been set against that.)
+    const bool kv8 = c->kv8_on && model == DEER_TARGET;
     const bool slim = c->slim && !mc.n_experts && ntiles <= SLIM_TILES && d <= SLIM_MAX_D;
     const int ssq_sub = m.ssq_sub == 4 ? 4 : slim ? 2 : 1;   // what the pass's residual GEMMs leave: one sum of squares per 32, 64 or 128 columns
     hipStream_t s = c->stream;
@@ -825,14 +871,22 @@ int run_pass(deer_ctx *c, int model, int ntiles, int n_attn, int max_limit, cons
         a.kv = KvView{m.kv + m.kv_k_base + (size_t)l * m.kv_layer_stride, m.kv + m.kv_v_base + (size_t)l * m.kv_layer_stride,
                       m.kv_seq_stride, m.kv_head_stride, c->p.max_seq};
         // whole key tiles that no row of this pass writes (a pass of one tile appends at most 32 rows)
-        if (fetch_ahead && NS_head > 0 && c->batch == 1 && 8 % mc.n_kv_heads == 0)
+        if (kv8) {
+            const Kv8Hot hot = c->kv8.hot_view(l);
+            a.kv = KvView{hot.k, hot.v, hot.seq_stride, hot.head_stride, c->p.max_seq};
+        } else if (fetch_ahead && NS_head > 0 && c->batch == 1 && 8 % mc.n_kv_heads == 0)
             a.kv_fetch_bytes = std::min(KV_FETCH_MAX_BYTES, std::max(0, (max_limit - 32) / 32) * 32 * hd * 2);
         if (kv_only(l)) { a.Hq = 0; a.kv_fetch_bytes = 0; }
         int rc = launch_gemm<EPI_QKV>(c, a, d, ntiles, 0);
         if (rc) return rc;
+        if (kv8) {
+            prof_close(c);
+            HIPCHK(c, kv8_settle(c->kv8, c->stream, l));
+        }
         if (kv_only(l)) break;
         const NextWeights nx_o = fetch_ahead_narrow ? next_plan_narrow(lw + m.lo_o, d, m.kattn, 1) : next_plan(lw + m.lo_o, d, m.kattn, EPI_RESID);
-        if (hd == 128) rc = launch_attn<128>(c, m, l, n_attn, NS, NS_head, scale_log2e, kv_bytes, nx_o);
+        if (kv8) rc = launch_attn_kv8(c, l, kv_bytes / 2, rows_desc);
+        else if (hd == 128) rc = launch_attn<128>(c, m, l, n_attn, NS, NS_head, scale_log2e, kv_bytes, nx_o);
         else if (hd == 64) rc = launch_attn<64>(c, m, l, n_attn, NS, NS_head, scale_log2e, kv_bytes, nx_o);
         else rc = launch_attn<32>(c, m, l, n_attn, NS, NS_head, scale_log2e, kv_bytes, nx_o);
         if (rc) return rc;
@@ -945,7 +999,7 @@ void fill_state(deer_ctx *c, char *img, int B, const int *len, const int *dr_len
     memset(img + ((char *)c->wk.st.ing_n - up), 0, (size_t)B * 4);
     memset(img + ((char *)c->wk.st.finished - up), 0, (size_t)B * 4);
 }
-struct PrefillPass { std::vector<int4> desc; int n_rows = 0, maxlim = 0; };   // attention tiles (see PassRows), GEMM rows, most visible keys
+struct PrefillPass { std::vector<int4> desc; int n_rows = 0, maxlim = 0, max_new = 0; };   // attention tiles (see PassRows), GEMM rows, most visible keys, most rows of a sequence
 // The uploads and passes of a prefill; passes[model] and ids must live until the stream has been waited for.
 int enqueue_prefill(deer_ctx *c, int batch, const int *ids, const int *lens, const int *pending, size_t total,
                     const std::vector<PrefillPass> (&passes)[2]) {
@@ -969,6 +1023,8 @@ int enqueue_prefill(deer_ctx *c, int batch, const int *ids, const int *lens, con
     for (const PrefillPass &pa : passes[DEER_DRAFTER]) fits = fits && (pa.n_rows + 31) / 32 <= BESIDE_TILES;
     const bool beside = fits && c->side && !c->prof_on && c->stamp_launch < 0;
     if (beside) HIPCHK(c, hipEventRecord(c->fork, c->stream));
+    if (c->kv8_on)   // every sequence's pages go back to the pool
+        HIPCHK(c, kv8_reserve(c->kv8, c->stream, nullptr, 0, nullptr, 0, c->p.max_batch, 0, 0, 0));
     auto run = [&](int model) -> int {
         for (size_t i = 0; i < passes[model].size(); ++i) {
             const PrefillPass &pa = passes[model][i];
@@ -977,6 +1033,15 @@ int enqueue_prefill(deer_ctx *c, int batch, const int *ids, const int *lens, con
             PassRows pr{};
             pr.kind = ROWS_PREFILL; pr.desc = w.pf_desc[model]; pr.ids = w.ids; pr.n_desc = (int)pa.desc.size();
             const LmPlan lm{false, 0, 0, 0.f, 0};
+            if (c->kv8_on && model == DEER_TARGET) {
+                Kv8Cache &k = c->kv8;
+                hipLaunchKernelGGL(k_kv8_prompt_pass, dim3(1), dim3(1024), 0, c->stream, w.pf_desc[model], pr.n_desc, k.st.len, batch, k.ask_start, k.ask_count, k.ask_row0);
+                LAUNCHCHK(c, "k_kv8_prompt_pass");
+                // (sequences without rows in this pass may hold more tokens than those with some)
+                HIPCHK(c, kv8_reserve(k, c->stream, k.ask_start, 0, k.ask_count, 0, batch, pa.n_rows, pa.max_new, k.p.max_seq));
+                k.max_len = pa.maxlim;
+                kv8_place(c, pr);
+            }
             if (int rc = run_pass(c, model, (pa.n_rows + 31) / 32, pr.n_desc, pa.maxlim, lm, 0.0, pr)) return rc;
         }
         return DEER_OK;
@@ -1013,14 +1078,20 @@ extern "C" {
 
 int deer_query_sizes(const deer_init_params *p, deer_sizes *out) {
     if (!out) return fail(nullptr, DEER_EINVAL, "null output");
-    if (p && (p->struct_size != sizeof(deer_init_params) || p->abi_version != DEER_ABI_VERSION))
-        return fail(nullptr, DEER_EVERSION, "struct_size/abi_version mismatch");
+    deer_init_params full;
+    if (p && !read_params(p, full)) return fail(nullptr, DEER_EVERSION, "struct_size/abi_version mismatch");
+    if (p) p = &full;
     if (const char *e = check_params(p)) return fail(nullptr, DEER_EINVAL, "%s", e);
     ModelRT m;
     for (int i = 0; i < 2; ++i) {
         plan_model(m, i == 0 ? p->target : p->drafter, p->max_batch, p->max_seq);
         out->weights[i] = m.weight_bytes;
         out->kv[i] = m.kv_bytes;
+    }
+    if (p->target_kv_format == DEER_KV_E4M3) {
+        Kv8Cache c;
+        plan_kv8(c, target_kv8_shape(*p), nullptr, nullptr);
+        out->kv[DEER_TARGET] = c.cache_bytes + c.work_bytes;
     }
     Work w;
     plan_work(w, *p, nullptr);
@@ -1035,6 +1106,9 @@ int deer_init_models(const deer_init_params *p, const deer_buffers *bufs, const 
     deer_sizes need;
     int rc = deer_query_sizes(p, &need);
     if (rc) return rc;
+    deer_init_params full;
+    read_params(p, full);
+    p = &full;
     for (int i = 0; i < 2; ++i) {
         if (!bufs->weights[i] || !bufs->kv[i]) return fail(nullptr, DEER_EINVAL, "null device buffer");
         if (buf_sizes->weights[i] < need.weights[i] || buf_sizes->kv[i] < need.kv[i])
@@ -1064,9 +1138,15 @@ int deer_init_models(const deer_init_params *p, const deer_buffers *bufs, const 
     }
     plan_work(c->wk, *p, (char *)bufs->workspace);
     c->max_tiles = std::max(2 * p->max_batch, PREFILL_TILES);
+    if (p->target_kv_format == DEER_KV_E4M3) {
+        c->kv8_on = true;
+        Kv8Cache sizes;
+        plan_kv8(sizes, target_kv8_shape(*p), nullptr, nullptr);
+        plan_kv8(c->kv8, target_kv8_shape(*p), (char *)bufs->kv[DEER_TARGET], (char *)bufs->kv[DEER_TARGET] + sizes.cache_bytes);
+    }
     // caches must hold finite values everywhere: masked keys are multiplied by zero weights
     for (int i = 0; i < 2; ++i) {
-        e = hipMemsetAsync(bufs->kv[i], 0, need.kv[i], c->stream);
+        e = c->kv8_on && i == DEER_TARGET ? kv8_clear(c->kv8, c->stream) : hipMemsetAsync(bufs->kv[i], 0, need.kv[i], c->stream);
         if (e != hipSuccess) { delete c; return fail(nullptr, DEER_EHIP, "hipMemsetAsync: %s", hipGetErrorString(e)); }
         const deer_model_cfg &mc = c->m[i].c;
         double th[64];
@@ -1175,20 +1255,27 @@ int deer_prefill(deer_ctx *c, int32_t batch, const int32_t *ids, const int32_t *
     // as fit, and its GEMM rows follow each other without gaps (rows of one sequence that are split over passes continue in
     // the next pass, over the keys the earlier pass has written).  The buffers hold PREFILL_TILES tiles, and what a draft pass
     // of max_batch sequences needs: many short prompts of a large batch then go through in fewer passes.
+    // (An 8-bit cache: the two tiles of a page stay in one pass.)
+    if (c->kv8_on && !kv8_fits(c, batch, [&](int b) { return lens[b] - 1; }))
+        return fail(c, DEER_ECAPACITY, "the prompts need more than the %d pages of the target's cache", c->kv8.p.n_pages);
     const int cap = c->max_tiles;
     std::vector<PrefillPass> passes[2];
     for (int model = 0; model < 2; ++model)
         for (int b = 0; b < batch; ++b) {
             const int nrows = (model == DEER_TARGET) ? lens[b] - 1 : lens[b];   // the last token stays pending for the target
+            int new_rows = 0;   // of this sequence in the pass
             for (int c0 = 0; c0 < nrows;) {
                 std::vector<PrefillPass> &ps = passes[model];
-                if (ps.empty() || (int)ps.back().desc.size() == cap) ps.emplace_back();
+                const bool page = c->kv8_on && model == DEER_TARGET && c0 % KV8_PAGE == 0 && nrows - c0 > 32;
+                if (ps.empty() || (int)ps.back().desc.size() + page >= cap) ps.emplace_back();
                 PrefillPass &pa = ps.back();
                 const int take = std::min(nrows - c0, 32);
                 pa.desc.push_back(make_int4(b, c0, take | pa.n_rows << 6, (int)(offs[b] + c0)));
                 pa.maxlim = std::max(pa.maxlim, c0 + take);
                 c0 += take;
                 pa.n_rows += take;
+                new_rows = pa.desc.size() > 1 && pa.desc[pa.desc.size() - 2].x == b ? new_rows + take : take;
+                pa.max_new = std::max(pa.max_new, new_rows);
             }
         }
     c->state = ST_INIT;   // no sequences until all of the call has worked: the device state may be of the new ones, the host's of the old
@@ -1208,6 +1295,24 @@ int deer_set_prefilled(deer_ctx *c, int32_t batch, const int32_t *lens, const in
         if (lens[b] < 1) return fail(c, DEER_EINVAL, "sequence %d is empty", b);
         if (lens[b] + c->p.max_k > c->p.max_seq) return fail(c, DEER_ECAPACITY, "sequence %d exceeds max_seq", b);
         if (last[b] < 0 || last[b] >= c->p.target.vocab) return fail(c, DEER_EINVAL, "token id outside the vocabulary");
+    }
+    std::vector<int> ask;
+    if (c->kv8_on) {   // the target's rows must be there, and the open page's in the ring
+        std::vector<int> at(2 * (size_t)batch);
+        HIPCHK(c, hipMemcpyAsync(at.data(), c->kv8.st.len, (size_t)batch * 4, hipMemcpyDeviceToHost, c->stream));
+        HIPCHK(c, hipMemcpyAsync(at.data() + batch, c->kv8.st.hot, (size_t)batch * 4, hipMemcpyDeviceToHost, c->stream));
+        HIPCHK(c, hipStreamSynchronize(c->stream));
+        for (int b = 0; b < batch; ++b) {
+            const int n = lens[b] - 1;
+            if (n > at[b] || (n % KV8_PAGE && n / KV8_PAGE < at[batch + b]))
+                return fail(c, DEER_EINVAL, "sequence %d: the target's 8-bit cache does not hold tokens 0 .. %d, or their last page only in 8 bits (deer_debug_load_kv)", b, n - 1);
+        }
+        c->state = ST_INIT;   // (see deer_prefill)
+        ask.assign(c->p.max_batch, 0);   // the other sequences' pages go back to the pool
+        for (int b = 0; b < batch; ++b) ask[b] = lens[b] - 1;
+        HIPCHK(c, hipMemcpyAsync(c->kv8.ask_start, ask.data(), ask.size() * 4, hipMemcpyHostToDevice, c->stream));
+        const hipError_t e = kv8_reserve(c->kv8, c->stream, c->kv8.ask_start, 0, nullptr, 0, c->p.max_batch, 0, 0, c->kv8.p.max_seq);
+        if (e != hipSuccess) { (void)hipStreamSynchronize(c->stream); return fail(c, DEER_EHIP, "state: %s", hipGetErrorString(e)); }
     }
     const size_t bytes = c->wk.up_desc;
     char *img = upload_image(c, bytes);
@@ -1233,6 +1338,8 @@ int deer_draft_block_multipass(deer_ctx *c, int32_t k, float T, uint64_t seed, i
         n_ing += c->h_ing_n[b];
         max_ing = std::max(max_ing, c->h_ing_n[b]);
     }
+    if (c->kv8_on && !kv8_fits(c, B, [&](int b) { return c->h_len[b] - 1 + k + c->bonus; }))
+        return fail(c, DEER_ECAPACITY, "the block needs more than the %d pages of the target's cache", c->kv8.p.n_pages);
     Work &w = c->wk;
     double keys = 0;
     for (int b = 0; b < B; ++b) keys += c->h_len[b] + k;
@@ -1276,6 +1383,10 @@ int deer_verify_block(deer_ctx *c, int32_t k, float T, const int32_t *draft_dev)
     LmPlan lm{true, B * nrows, nrows, T, 0};
     double keys = 0;
     for (int b = 0; b < B; ++b) keys += c->h_len[b] - 1 + nrows;
+    if (c->kv8_on) {
+        HIPCHK(c, kv8_reserve(c->kv8, c->stream, w.st.len, -1, nullptr, nrows, B, B * nrows, nrows, maxlim));
+        kv8_place(c, pr);
+    }
     int rc = run_pass(c, DEER_TARGET, (B * nrows + 31) / 32, B, maxlim, lm, keys, pr);
     if (rc) return rc;
     c->wk_draft = draft_dev;
@@ -1520,6 +1631,30 @@ int deer_debug_load_kv(deer_ctx *c, int model, int32_t layer, int32_t seq, int32
     if (layer < 0 || layer >= m.c.n_layers || seq < 0 || seq >= c->p.max_batch) return fail(c, DEER_EINVAL, "layer or sequence out of range");
     if (first_slot < 0 || n_slots < 0 || (int64_t)first_slot + n_slots > c->p.max_seq) return fail(c, DEER_ECAPACITY, "slots %d .. %d exceed max_seq %d", first_slot, first_slot + n_slots, c->p.max_seq);
     if (n_slots == 0) return DEER_OK;
+    if (c->kv8_on && model == DEER_TARGET) {
+        Kv8Cache &k = c->kv8;
+        int len = 0;
+        HIPCHK(c, hipMemcpyAsync(&len, k.st.len + seq, 4, hipMemcpyDeviceToHost, c->stream));
+        HIPCHK(c, hipStreamSynchronize(c->stream));
+        if (first_slot > len || (first_slot != len && first_slot % KV8_PAGE)) return fail(c, DEER_EINVAL, "an 8-bit cache takes slots from a multiple of 64 or from its %d tokens on", len);
+        if (!aligned16(k_rows_dev) || !aligned16(v_rows_dev)) return fail(c, DEER_EINVAL, "unaligned pointer");
+        c->state = ST_INIT;   // the cache is no longer that of the sequences (pages that a call gives back are the first that the next one takes)
+        const size_t width = (size_t)k.p.n_kv_heads * k.p.head_dim;
+        const int step = k.p.max_rows / KV8_PAGE * KV8_PAGE;
+        for (int at = 0; at < n_slots; at += step) {
+            const int n = std::min(step, n_slots - at);
+            hipLaunchKernelGGL(k_kv8_one, dim3((k.p.max_batch + 255) / 256), dim3(256), 0, c->stream, k.st.len, k.p.max_batch, seq, first_slot + at, n, k.ask_start, k.ask_count);
+            LAUNCHCHK(c, "k_kv8_one");
+            HIPCHK(c, kv8_reserve(k, c->stream, k.ask_start, 0, k.ask_count, 0, k.p.max_batch, n, n, k.p.max_seq));
+            HIPCHK(c, kv8_write(k, c->stream, layer, (const uint16_t *)k_rows_dev + at * width, (const uint16_t *)v_rows_dev + at * width, width, width));
+            HIPCHK(c, kv8_settle(k, c->stream, layer));
+        }
+        int st[2];
+        HIPCHK(c, hipMemcpyAsync(st, k.st.stat, sizeof st, hipMemcpyDeviceToHost, c->stream));
+        HIPCHK(c, hipStreamSynchronize(c->stream));
+        if (st[1]) return fail(c, DEER_ECAPACITY, "the pages of the target's cache do not suffice for %d slots of sequence %d", first_slot + n_slots, seq);
+        return DEER_OK;
+    }
     const KvView kv{m.kv + m.kv_k_base + (size_t)layer * m.kv_layer_stride, m.kv + m.kv_v_base + (size_t)layer * m.kv_layer_stride,
                     m.kv_seq_stride, m.kv_head_stride, c->p.max_seq};
     const size_t items = (size_t)n_slots * m.c.n_kv_heads * (m.c.head_dim / 8);
@@ -1536,7 +1671,7 @@ int deer_get_lengths(const deer_ctx *c, int32_t *len) {
 }
 
 int deer_get_kv_layout(const deer_ctx *c, int model, deer_kv_layout *out) {
-    if (!c || !out || model < 0 || model > 1) return DEER_EINVAL;
+    if (!c || !out || model < 0 || model > 1 || (c->kv8_on && model == DEER_TARGET)) return DEER_EINVAL;   // (pages have no such layout)
     const ModelRT &m = c->m[model];
     out->k_base = m.kv_k_base; out->v_base = m.kv_v_base;
     out->layer_stride = m.kv_layer_stride; out->seq_stride = m.kv_seq_stride; out->head_stride = m.kv_head_stride;
@@ -1584,7 +1719,6 @@ Kv8Shape kv8_shape(const deer_kv8_params *p) {
 // a row stride in elements that keeps 16-byte loads aligned, over rows of at least `width`
 bool kv8_stride_ok(int64_t stride, int64_t width, int dtype) { return stride >= width && stride % (dtype == DEER_F32 ? 4 : 8) == 0 && stride < (int64_t)1 << 32; }
 bool kv8_dtype_ok(int dtype) { return dtype == DEER_F32 || dtype == DEER_BF16; }
-bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
 bool aligned4(const void *p) { return ((uintptr_t)p & 3) == 0; }
 
 }  // namespace

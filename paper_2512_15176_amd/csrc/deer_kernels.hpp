@@ -347,6 +347,7 @@ struct PassRows {
     int mask_id, n_fixed;
     int B, share, n_ingest;          // sequences; draft: committed tokens in all that the drafter has not cached
     const int4 *desc; const int *ids; int n_desc;   // prefill
+    const int *slot_base; int slot_mask;            // where a row's K and V go: (slot + slot_base[sequence]) & slot_mask; null: its slot
 };
 struct RowDesc { int tok, pos, slot, seq, qrow; };
 
@@ -510,7 +511,7 @@ __global__ __launch_bounds__(256) void k_pass_begin(PassRows p, RowMeta rm, cons
         const int row = t * 32 + threadIdx.x;
         const RowDesc r = pass_row(p, s_pref, row);
         s_tok[threadIdx.x] = r.tok; s_pos[threadIdx.x] = r.pos;
-        if ((int)blockIdx.x == ncg) { rm.pos[row] = r.pos; rm.slot[row] = r.slot; rm.seq[row] = r.seq; rm.qrow[row] = r.qrow; }
+        if ((int)blockIdx.x == ncg) { rm.pos[row] = r.pos; rm.slot[row] = p.slot_base && r.slot >= 0 ? (r.slot + p.slot_base[r.seq]) & p.slot_mask : r.slot; rm.seq[row] = r.seq; rm.qrow[row] = r.qrow; }
     }
     __syncthreads();
     if ((int)blockIdx.x < ncg) {

@@ -164,6 +164,27 @@ __global__ __launch_bounds__(1024) void k_kv8_reserve(Kv8State s, const int *__r
     if (b == 0) { s.stat[0] = top + given - taken; s.stat[1] = s_refused; }
 }
 
+// The requests of a prompt pass, from its attention tiles (see PassRows; the tiles of a sequence follow each other): sequences
+// without a tile keep what they hold.  row0: attention row of a sequence's first.  One workgroup of 1024.
+__global__ __launch_bounds__(1024) void k_kv8_prompt_pass(const int4 *__restrict__ desc, int n_desc, const int *__restrict__ len, int B, int *__restrict__ start,
+                                                          int *__restrict__ count, int *__restrict__ row0) {
+    for (int b = threadIdx.x; b < B; b += 1024) { start[b] = len[b]; count[b] = 0; row0[b] = 0; }
+    __syncthreads();
+    for (int t = threadIdx.x; t < n_desc; t += 1024) {
+        const int4 d = desc[t];
+        if (t == 0 || desc[t - 1].x != d.x) {
+            int n = 0;
+            for (int u = t; u < n_desc && desc[u].x == d.x; ++u) n += desc[u].z & 63;
+            start[d.x] = d.y; count[d.x] = n; row0[d.x] = t * 32;
+        }
+    }
+}
+// The request of one sequence; the others keep what they hold.
+__global__ void k_kv8_one(const int *__restrict__ len, int B, int b, int first, int n, int *__restrict__ start, int *__restrict__ count) {
+    const int i = blockIdx.x * blockDim.x + threadIdx.x;
+    if (i < B) { start[i] = i == b ? first : len[i]; count[i] = i == b ? n : 0; }
+}
+
 // ------------------------------------------------------------------------------------------
 // append
 // ------------------------------------------------------------------------------------------
@@ -412,7 +433,7 @@ struct Kv8Attn {
     const void *q; void *out;                      // rows
     long long q_stride, out_stride;                // elements
     const uint4 *qhi, *qlo; uint4 *xhi, *xlo;      // fragments
-    const int *q_row0;                             // fragments: attention row of a sequence's first row
+    const int *q_row0;                             // fragments: attention row of a sequence's first row; null: 32 * sequence
     float *part;
     int Hq, Hkv, G, rows, NS, rts;                 // NS key ranges; rts: tiles of 32 packed rows per sequence
     float scale_log2e, m_init;
@@ -484,7 +505,7 @@ __device__ __forceinline__ void kv8_load_q(const Kv8Attn &a, const Kv8Row &r, in
             split_planes<3>(v, pl);
             q[0][s] = pl[0]; q[1][s] = pl[1]; q[2][s] = pl[2];
         } else {
-            const int ar = r.row < 0 ? 0 : a.q_row0[b] + r.row - a.s.cu[b];
+            const int ar = r.row < 0 ? 0 : (a.q_row0 ? a.q_row0[b] : 32 * b) + r.row - a.s.cu[b];
             const size_t vec = ((size_t)((ar >> 5) * a.Hq + r.head) * KSQ + s) * 64 + half * 32 + (ar & 31);
             q[0][s] = r.row < 0 ? zero : a.qhi[vec];
             q[1][s] = r.row < 0 ? zero : a.qlo[vec];

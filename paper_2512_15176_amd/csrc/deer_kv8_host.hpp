@@ -20,6 +20,7 @@ struct Kv8Cache {
     uint8_t *pages = nullptr;
     float *scales = nullptr, *part = nullptr;
     uint16_t *ring = nullptr, *scratch = nullptr;
+    int *ask_start = nullptr, *ask_count = nullptr, *ask_row0 = nullptr;   // requests that the library makes up itself, [max_batch]
     size_t scratch_slots = 0, cache_bytes = 0, work_bytes = 0;
     // the pass
     int batch = 0, rows = 0, max_new = 0, max_len = 0;
@@ -72,6 +73,7 @@ inline void plan_kv8(Kv8Cache &c, const Kv8Shape &p, char *cache, char *work) {
     off = 0; base = work;
     s.start = (int *)take(p.max_batch * 4); s.count = (int *)take(p.max_batch * 4); s.hotbase = (int *)take(p.max_batch * 4); s.carry = (int *)take(p.max_batch * 4);
     s.cu = (int *)take((p.max_batch + 1) * 4);
+    c.ask_start = (int *)take(p.max_batch * 4); c.ask_count = (int *)take(p.max_batch * 4); c.ask_row0 = (int *)take(p.max_batch * 4);
     s.slot = (int *)take((size_t)p.max_rows * 4); s.row_seq = (int *)take((size_t)p.max_rows * 4); s.row_pos = (int *)take((size_t)p.max_rows * 4);
     // a sequence's rows of a long pass touch whole pages: up to 127 slots more than rows
     c.scratch_slots = p.max_rows > KV8_PAGE ? ((size_t)p.max_rows + (size_t)std::min(p.max_batch, p.max_rows) * 127 + 63) / 64 * 64 : 0;

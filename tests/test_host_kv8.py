@@ -126,3 +126,68 @@ assert lib.deer_kv8_append(kv, 0, None, None, 1, 0, 0, 0) == 0 and lib.deer_kv8_
 print([n for n, g in launches()])
 """)
     assert out.count("k_kv8") == 1 and "k_kv8_reserve" in out
+
+
+def _engine_rc(**kw):
+    import deer_inputs as di
+    cfg = di.CONFIGS["tiny"]
+    p = binding.init_params(cfg["target"], cfg["drafter"], 2, kw.pop("max_seq", 256), 8, 0, **kw)
+    s = binding.Sizes()
+    return binding.load_library().deer_query_sizes(C.byref(p), C.byref(s)), s, p
+
+
+def test_an_engine_takes_the_format():
+    rc, plain, p = _engine_rc()
+    assert rc == 0
+    p.struct_size = binding.InitParams.target_kv_format.offset          # a caller that does not know of it
+    p.target_kv_format = 77
+    s = binding.Sizes()
+    assert binding.load_library().deer_query_sizes(C.byref(p), C.byref(s)) == 0 and s.kv[0] == plain.kv[0]
+    rc, e8, _ = _engine_rc(kv_format=1)
+    assert rc == 0 and e8.kv[1] == plain.kv[1] and e8.workspace == plain.workspace and e8.kv[0] != plain.kv[0]
+    assert _engine_rc(kv_format=2)[0] == -1 and _engine_rc(kv_format=1, kv_pages=-1)[0] == -1
+    assert _engine_rc(kv_format=1, max_seq=(1 << 20) + 64)[0] == -1
+
+
+def test_an_engine_of_long_contexts_needs_half_the_memory():
+    import deer_inputs as di
+    cfg = di.CONFIGS["qwen3_8b_long_batch"]
+    sizes = []
+    for fmt in (0, 1):
+        p = binding.init_params(cfg["target"], cfg["drafter"], 16, 32768 + 64, 32, 0, kv_format=fmt)
+        s = binding.Sizes()
+        assert binding.load_library().deer_query_sizes(C.byref(p), C.byref(s)) == 0
+        sizes.append(s.kv[0])
+    assert sizes[1] < 0.53 * sizes[0]
+
+
+def test_an_engine_settles_pages_and_attends_in_8_bits(tmp_path):
+    out = run(tmp_path, """
+import deer_inputs as di
+cfg = di.CONFIGS["tiny"]
+t = di.scaled(cfg["target"], n_layers=5)
+p = B.init_params(t, cfg["drafter"], 2, 256, 8, t.vocab - 1, kv_format=1, kv_pages=4)
+s = B.query_sizes(p)
+bufs = B.Buffers((C.c_void_p * 2)(*[buf(n) for n in s.weights]), (C.c_void_p * 2)(*[buf(n) for n in s.kv]), buf(s.workspace))
+ctx = C.c_void_p()
+assert lib.deer_init_models(C.byref(p), C.byref(bufs), C.byref(s), C.byref(ctx)) == 0
+I32 = lambda v: (C.c_int32 * len(v))(*v)
+pre = lambda lens: lib.deer_prefill(ctx, len(lens), I32([3] * sum(lens)), I32(lens))
+assert pre([130, 130]) == -3                     # six pages of four
+launches()
+assert pre([130, 60]) == 0
+names = [n for n, g in launches()]
+count = lambda what: sum(what in n for n in names)
+assert count("k_kv8_reserve") == 2 and count("k_kv8_prompt_pass") == 1
+assert count("k_kv8_settle") == 5 and count("k_kv8_attn") == 4      # the last layer ends with its K and V rows
+draft = (C.c_int32 * 64)()
+assert lib.deer_draft_block(ctx, 8, C.c_float(0.0), 0, draft) == -3     # 129 + 8 and 59 + 8 tokens: 3 + 2 pages
+assert lib.deer_draft_block(ctx, 5, C.c_float(0.0), 0, draft) == 0
+launches()
+assert lib.deer_verify_block(ctx, 5, C.c_float(0.0), draft) == 0
+names = [n for n, g in launches()]
+assert count("k_kv8_reserve") == 1 and count("k_kv8_settle") == 5 and count("k_kv8_attn") == 5
+assert not any("k_attn" in n for n in names)
+print("done")
+""")
+    assert "done" in out
