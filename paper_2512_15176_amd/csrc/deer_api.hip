@@ -1646,8 +1646,7 @@ int deer_debug_load_kv(deer_ctx *c, int model, int32_t layer, int32_t seq, int32
             hipLaunchKernelGGL(k_kv8_one, dim3((k.p.max_batch + 255) / 256), dim3(256), 0, c->stream, k.st.len, k.p.max_batch, seq, first_slot + at, n, k.ask_start, k.ask_count);
             LAUNCHCHK(c, "k_kv8_one");
             HIPCHK(c, kv8_reserve(k, c->stream, k.ask_start, 0, k.ask_count, 0, k.p.max_batch, n, n, k.p.max_seq));
-            HIPCHK(c, kv8_write(k, c->stream, layer, (const uint16_t *)k_rows_dev + at * width, (const uint16_t *)v_rows_dev + at * width, width, width));
-            HIPCHK(c, kv8_settle(k, c->stream, layer));
+            HIPCHK(c, kv8_append(k, c->stream, layer, (const uint16_t *)k_rows_dev + at * width, (const uint16_t *)v_rows_dev + at * width, width, width));
         }
         int st[2];
         HIPCHK(c, hipMemcpyAsync(st, k.st.stat, sizeof st, hipMemcpyDeviceToHost, c->stream));
@@ -1781,9 +1780,8 @@ int deer_kv8_append(deer_kv8 *c, int32_t layer, const void *k_dev, const void *v
     if (!kv8_stride_ok(k_stride, width, dtype) || !kv8_stride_ok(v_stride, width, dtype)) return fail8(c, DEER_EINVAL, "row strides must cover the heads and keep 16-byte alignment");
     DeviceScope dev(c->device);
     KV8CHK(c, dev.err);
-    if (dtype == DEER_F32) KV8CHK(c, kv8_write(c->c, c->stream, layer, (const float *)k_dev, (const float *)v_dev, (size_t)k_stride, (size_t)v_stride));
-    else KV8CHK(c, kv8_write(c->c, c->stream, layer, (const uint16_t *)k_dev, (const uint16_t *)v_dev, (size_t)k_stride, (size_t)v_stride));
-    KV8CHK(c, kv8_settle(c->c, c->stream, layer));
+    if (dtype == DEER_F32) KV8CHK(c, kv8_append(c->c, c->stream, layer, (const float *)k_dev, (const float *)v_dev, (size_t)k_stride, (size_t)v_stride));
+    else KV8CHK(c, kv8_append(c->c, c->stream, layer, (const uint16_t *)k_dev, (const uint16_t *)v_dev, (size_t)k_stride, (size_t)v_stride));
     return DEER_OK;
 }
 
@@ -1819,11 +1817,10 @@ int deer_kv8_read(deer_kv8 *c, int32_t layer, const int32_t *seq_dev, const int3
     if (n == 0) return DEER_OK;
     if (!seq_dev || !pos_dev || !k_dev || !v_dev || !aligned4(seq_dev) || !aligned4(pos_dev) || !aligned16(k_dev) || !aligned16(v_dev))
         return fail8(c, DEER_EINVAL, "null or unaligned pointer");
-    const size_t items = (size_t)n * p.n_kv_heads * (p.head_dim / 8);
-    if ((items + 255) / 256 > 0x7fffffffu) return fail8(c, DEER_EINVAL, "too many rows for one call");
+    const size_t items = (size_t)n * (p.head_dim / 8);
     DeviceScope dev(c->device);
     KV8CHK(c, dev.err);
-    const dim3 grid((unsigned)((items + 255) / 256));
+    const dim3 grid((unsigned)((items + 255) / 256), p.n_kv_heads);
     const Kv8Hot ring = c->c.ring_view(layer);
     if (dtype == DEER_F32)
         hipLaunchKernelGGL(k_kv8_read<float>, grid, dim3(256), 0, c->stream, c->c.st, seq_dev, pos_dev, n, ring, c->c.layer_pages(layer), c->c.layer_scales(layer),

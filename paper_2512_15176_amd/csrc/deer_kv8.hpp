@@ -207,73 +207,6 @@ __device__ __forceinline__ bool nonfinite8(uint4 v) {
     return bad;
 }
 
-// Rows of the pass [row][kv head][head_dim] into the hot pages.  A token with an infinity or NaN in its K or V row of a head gets a key
-// of NaNs and a value of zeros there: rows that see it come out NaN, and rows that do not, whose weight for it is zero, do not meet
-// 0 x NaN.  One thread per (row, head, octet); the octets of a head are neighbouring lanes.
-// The workgroups behind those, one per (sequence, kv head), bring the open page's older rows to where the pass's are, and to the kept
-// page if the pass is a long one (its last pages may take that half of the ring).  Only elements of older tokens are written.
-template <typename SrcT>
-__global__ __launch_bounds__(256) void k_kv8_write(Kv8State s, const SrcT *__restrict__ k, const SrcT *__restrict__ v, size_t k_stride,
-                                                   size_t v_stride, Kv8Hot hot, Kv8Hot ring, int rows, int row_wgs, int Hkv, int hd) {
-    const int octs = hd >> 3;
-    if ((int)blockIdx.x >= row_wgs) {
-        const int item = blockIdx.x - row_wgs, b = item / opaque_s(Hkv), head = item % opaque_s(Hkv), from = s.carry[b];
-        if (from == 0) return;
-        const int st = s.start[b], page = st / KV8_PAGE, old = st % KV8_PAGE;
-        const size_t kept = (size_t)b * ring.seq_stride + (size_t)head * ring.head_stride + (size_t)KV8_RING * hd;
-        const size_t src = from == 2 ? kept : (size_t)b * ring.seq_stride + (size_t)head * ring.head_stride + (size_t)((page * KV8_PAGE) & ring.mask) * hd;
-        const size_t dst = (size_t)b * hot.seq_stride + (size_t)head * hot.head_stride + (size_t)((page * KV8_PAGE + s.hotbase[b]) & hot.mask) * hd;
-        const bool keep = from == 1;      // (1 only where the pass is long)
-        for (int i = threadIdx.x; i < old * octs; i += 256) {
-            const size_t at = k_cache_off(i / octs, i % octs, hd);
-            const uint4 x = *(const uint4 *)(ring.k + src + at);
-            *(uint4 *)(hot.k + dst + at) = x;
-            if (keep) *(uint4 *)(ring.k + kept + at) = x;
-        }
-        for (int i = threadIdx.x; i < (old + 7) / 8 * hd; i += 256) {      // eight tokens of a channel
-            const int o = i / hd * 8, c = i % hd;
-            const size_t at = v_cache_off(o, c, hd);
-            const uint4 x = *(const uint4 *)(ring.v + src + at);
-            if (o + 8 <= old) {
-                *(uint4 *)(hot.v + dst + at) = x;
-                if (keep) *(uint4 *)(ring.v + kept + at) = x;
-            } else {
-                const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-                for (int e = 0; e < 7; ++e)
-                    if (o + e < old) {
-                        const uint16_t y = (uint16_t)(w[e >> 1] >> (16 * (e & 1)));
-                        hot.v[dst + at + e] = y;
-                        if (keep) ring.v[kept + at + e] = y;
-                    }
-            }
-        }
-        return;
-    }
-    const size_t gid = (size_t)blockIdx.x * 256 + threadIdx.x;
-    const bool in = gid < (size_t)rows * Hkv * octs;
-    const int oct = (int)(gid % octs), head = (int)((gid / octs) % Hkv), r = in ? (int)(gid / ((size_t)octs * Hkv)) : 0;
-    const int b = in ? s.row_seq[r] : -1;
-    uint4 kk = make_uint4(0u, 0u, 0u, 0u), vv = kk;
-    if (b >= 0) {
-        kk = load8_bf16(k + (size_t)r * k_stride + (size_t)head * hd + oct * 8);
-        vv = load8_bf16(v + (size_t)r * v_stride + (size_t)head * hd + oct * 8);
-    }
-    const unsigned long long bad = __builtin_amdgcn_ballot_w64(nonfinite8(kk) || nonfinite8(vv));
-    const int lane = threadIdx.x & 63;
-    if ((bad >> (lane & ~(octs - 1))) & ((1ull << octs) - 1)) {
-        kk = make_uint4(0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u);
-        vv = make_uint4(0u, 0u, 0u, 0u);
-    }
-    if (b < 0) return;
-    const int slot = (s.row_pos[r] + s.hotbase[b]) & hot.mask;
-    const size_t base = (size_t)b * hot.seq_stride + (size_t)head * hot.head_stride;
-    *(uint4 *)(hot.k + base + k_cache_off(slot, oct, hd)) = kk;
-    const uint32_t w[4] = {vv.x, vv.y, vv.z, vv.w};
-#pragma unroll
-    for (int e = 0; e < 8; ++e) hot.v[base + v_cache_off(slot, oct * 8 + e, hd)] = (uint16_t)(w[e >> 1] >> (16 * (e & 1)));
-}
-
 // the scale of a page whose largest magnitude is amax: 2^e, smallest with amax <= 448 * 2^e = 1.75 * 2^(e + 8); 1 for a page of
 // zeros.  Not below 2^-100: what is smaller than 2^-109 then becomes zero.
 __device__ __forceinline__ float kv8_scale(float amax) {
@@ -300,79 +233,205 @@ __device__ __forceinline__ uint2 quant8(uint4 v, float inv) {
     }
     return make_uint2((uint32_t)o[0], (uint32_t)o[1]);
 }
-// After the rows of a pass are in the hot pages: every page that they complete is quantised into its place in the pool.  With the
-// rows in the scratch (ring.k not null) the last two pages go to the ring.
-// pages, scales: the layer's.  grid: x page of the sequence's pass, y kv head, z sequence; 256 threads, each with a chunk (two
-// fragments, 32 bytes of bf16) at a time; everything of the page is in registers between the maximum and the rounding.
+// A page's 64 rows of one head in registers, K and V in fragment order: thread t has the lanes' vectors of chunks t, t + 256, .. (two
+// fragments each).  They are quantised into the pool; 256 threads, all of which call it.
 template <int HD>
-__global__ __launch_bounds__(256) void k_kv8_settle(Kv8State s, Kv8Hot hot, Kv8Hot ring, uint8_t *__restrict__ pages, float *__restrict__ scales, int Hkv) {
-    constexpr int NC = KV8_PAGE * HD / 16;          // chunks of K, and of V
-    constexpr int PER = (NC + 255) / 256;
-    __shared__ float s_max[2][4];
-    const int b = blockIdx.z, head = blockIdx.y, n = s.count[b];
-    if (n == 0) return;
-    const int st = s.start[b], end = st + n, first = st / KV8_PAGE, last = (end - 1) / KV8_PAGE, page = first + blockIdx.x;
-    if (page > last) return;
-    const bool whole = end >= (page + 1) * KV8_PAGE;
-    const bool out = ring.k && page >= last - 1;
-    if (!whole && !out) return;
-    const size_t hb = (size_t)b * hot.seq_stride + (size_t)head * hot.head_stride + (size_t)((page * KV8_PAGE + s.hotbase[b]) & hot.mask) * HD;
-    const size_t rb = (size_t)b * ring.seq_stride + (size_t)head * ring.head_stride + (size_t)((page * KV8_PAGE) & ring.mask) * HD;
+struct Kv8Regs {
+    static constexpr int NC = KV8_PAGE * HD / 16;   // chunk lanes of K, and of V
+    static constexpr int PER = (NC + 255) / 256;
     uint4 x[2][PER][2];
+};
+template <int HD>
+__device__ __forceinline__ void kv8_quantise(const Kv8Regs<HD> &p, uint8_t *__restrict__ pp, float *__restrict__ scales, float (&s_max)[2][4]) {
+    using R = Kv8Regs<HD>;
     float amax[2] = {0.f, 0.f};
 #pragma unroll
     for (int kv = 0; kv < 2; ++kv) {
-        uint16_t *hp = (kv ? hot.v : hot.k) + hb, *rp = (kv ? ring.v : ring.k) + rb;
 #pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const int c = threadIdx.x + 256 * i, lane = c & 63, f0 = (c >> 6) * 2;
-            if (NC % 256 && c >= NC) continue;
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const size_t off = ((size_t)(f0 + u) * 64 + lane) * 8;
-                const uint4 v = *(const uint4 *)(hp + off);
-                if (out) *(uint4 *)(rp + off) = v;
-                amax[kv] = amax8(amax[kv], v);
-                x[kv][i][u] = v;
-            }
+        for (int i = 0; i < R::PER; ++i) {
+            if (R::NC % 256 && threadIdx.x + 256 * i >= R::NC) continue;
+            amax[kv] = amax8(amax8(amax[kv], p.x[kv][i][0]), p.x[kv][i][1]);
         }
-    }
-    if (!whole) return;      // (the whole workgroup)
-#pragma unroll
-    for (int kv = 0; kv < 2; ++kv) {
 #pragma unroll
         for (int off = 1; off < 64; off <<= 1) amax[kv] = fmaxf(amax[kv], shx(amax[kv], off));
         if ((threadIdx.x & 63) == 0) s_max[kv][threadIdx.x >> 6] = amax[kv];
     }
     __syncthreads();
-    const int id = s.table[(size_t)b * s.max_blocks + page];
-    if ((unsigned)id >= (unsigned)s.n_pages) return;
-    uint8_t *pp = pages + ((size_t)id * Hkv + head) * (2 * KV8_PAGE * HD);
 #pragma unroll
     for (int kv = 0; kv < 2; ++kv) {
         const float sc = kv8_scale(fmaxf(fmaxf(s_max[kv][0], s_max[kv][1]), fmaxf(s_max[kv][2], s_max[kv][3])));
         const float inv = __uint_as_float((254u << 23) - __float_as_uint(sc));    // 1 / 2^e
-        if (threadIdx.x == 0) scales[((size_t)id * Hkv + head) * 2 + kv] = sc;
+        if (threadIdx.x == 0) scales[kv] = sc;
 #pragma unroll
-        for (int i = 0; i < PER; ++i) {
+        for (int i = 0; i < R::PER; ++i) {
             const int c = threadIdx.x + 256 * i;
-            if (NC % 256 && c >= NC) continue;
-            const uint2 a = quant8(x[kv][i][0], inv), d = quant8(x[kv][i][1], inv);
+            if (R::NC % 256 && c >= R::NC) continue;
+            const uint2 a = quant8(p.x[kv][i][0], inv), d = quant8(p.x[kv][i][1], inv);
             *(uint4 *)(pp + (size_t)kv * KV8_PAGE * HD + (size_t)c * 16) = make_uint4(a.x, a.y, d.x, d.y);
         }
     }
 }
 
+// Where a page of a sequence and head lies.
+struct Kv8At { size_t hot, ring, kept; };      // elements
+__device__ __forceinline__ Kv8At kv8_at(const Kv8State &s, const Kv8Hot &hot, const Kv8Hot &ring, int b, int head, int page, int hd) {
+    const size_t rb = (size_t)b * ring.seq_stride + (size_t)head * ring.head_stride;
+    return Kv8At{(size_t)b * hot.seq_stride + (size_t)head * hot.head_stride + (size_t)((page * KV8_PAGE + s.hotbase[b]) & hot.mask) * hd,
+                 rb + (size_t)((page * KV8_PAGE) & ring.mask) * hd, rb + (size_t)KV8_RING * hd};
+}
+
+// A long pass that starts inside a page: the page's rows go from the ring to the kept page (the pass's last pages may take that half of
+// the ring, and the pass may be taken back).  grid: x kv head, y sequence; 256 threads
+template <int HD>
+__global__ __launch_bounds__(256) void k_kv8_keep(Kv8State s, Kv8Hot ring) {
+    const int b = blockIdx.y, head = blockIdx.x;
+    if (s.carry[b] != 1) return;
+    const Kv8At at = kv8_at(s, ring, ring, b, head, s.start[b] / KV8_PAGE, HD);
+    for (int i = threadIdx.x * 8; i < KV8_PAGE * HD; i += 256 * 8) {
+        *(uint4 *)(ring.k + at.kept + i) = *(const uint4 *)(ring.k + at.ring + i);
+        *(uint4 *)(ring.v + at.kept + i) = *(const uint4 *)(ring.v + at.ring + i);
+    }
+}
+
+// Rows of the pass [row][kv head][head_dim] enter the cache, one page of one head per workgroup: the rows become fragments (K's are the
+// rows' own octets; V goes through LDS, as a fragment has eight tokens of a channel), the page's older rows join them from the ring
+// or, behind a long pass's start or a pass taken back, from the kept page; the fragments go to the hot page, to the ring if the pass is long
+// and the page one of its last two, and, quantised, to the pool if the page is complete.
+// A token with an infinity or NaN in its K or V row of a head gets a key of NaNs and a value of zeros there: rows that see it come out
+// NaN, and rows that do not, whose weight for it is zero, do not meet 0 x NaN.
+// grid: x page of the sequence's pass, y kv head, z sequence; 256 threads
+template <int HD, typename SrcT>
+__global__ __launch_bounds__(256) void k_kv8_append(Kv8State s, const SrcT *__restrict__ k, const SrcT *__restrict__ v, size_t k_stride, size_t v_stride,
+                                                    Kv8Hot hot, Kv8Hot ring, int is_long, uint8_t *__restrict__ pages, float *__restrict__ scales, int Hkv) {
+    using R = Kv8Regs<HD>;
+    constexpr int OCTS = HD / 8, VS = HD + 8;       // padded row of V in LDS
+    __shared__ __attribute__((aligned(16))) uint16_t s_v[KV8_PAGE * VS];
+    __shared__ int s_bad[KV8_PAGE];
+    __shared__ float s_max[2][4];
+    const int b = blockIdx.z, head = blockIdx.y, n = s.count[b];
+    if (n == 0) return;
+    const int st = s.start[b], end = st + n, first = st / KV8_PAGE, last = (end - 1) / KV8_PAGE, page = first + blockIdx.x;
+    if (page > last) return;
+    const int t0 = max(st - page * KV8_PAGE, 0), t1 = min(end - page * KV8_PAGE, KV8_PAGE);    // the page's rows of this pass
+    const int row0 = s.cu[b] + page * KV8_PAGE - st;       // row of the page's token 0
+    const bool whole = t1 == KV8_PAGE, out = is_long && page >= last - 1;
+    const int carry = t0 > 0 ? s.carry[b] : 0;             // (0: the older rows are where they belong)
+    const Kv8At at = kv8_at(s, hot, ring, b, head, page, HD);
+    const size_t older = carry ? at.kept : at.ring;        // carry: the pass is long (kept by k_kv8_keep), or taken back
+    for (int i = threadIdx.x; i < KV8_PAGE; i += 256) s_bad[i] = 0;
+    __syncthreads();
+    for (int i = threadIdx.x; i < KV8_PAGE * OCTS; i += 256) {
+        const int tok = i / OCTS, oct = i % OCTS;
+        if (tok < t0 || tok >= t1) continue;
+        const uint4 x = load8_bf16(v + (size_t)(row0 + tok) * v_stride + (size_t)head * HD + oct * 8);
+        if (nonfinite8(x)) s_bad[tok] = 1;
+        *(uint4 *)(s_v + tok * VS + oct * 8) = x;
+    }
+    R p;
+#pragma unroll
+    for (int i = 0; i < R::PER; ++i) {
+        const int c = threadIdx.x + 256 * i, lane = c & 63, rr = lane & 31;
+        if (R::NC % 256 && c >= R::NC) continue;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int f = (c >> 6) * 2 + u, tok = f / (HD / 16) * 32 + 16 * ((rr >> 2) & 1) + 4 * (rr >> 3) + (rr & 3), oct = f % (HD / 16) * 2 + (lane >> 5);
+            uint4 x = make_uint4(0u, 0u, 0u, 0u);
+            if (tok >= t0 && tok < t1) {
+                x = load8_bf16(k + (size_t)(row0 + tok) * k_stride + (size_t)head * HD + oct * 8);
+                if (nonfinite8(x)) s_bad[tok] = 1;
+            } else if (tok < t0 && (whole || carry)) x = *(const uint4 *)(ring.k + older + ((size_t)f * 64 + lane) * 8);
+            p.x[0][i][u] = x;
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < R::PER; ++i) {
+        const int c = threadIdx.x + 256 * i, lane = c & 63, rr = lane & 31, half = lane >> 5;
+        if (R::NC % 256 && c >= R::NC) continue;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int f = (c >> 6) * 2 + u, blk = f / (HD / 16) * 32;
+            const size_t off = ((size_t)f * 64 + lane) * 8;
+            {
+                const int tok = blk + 16 * ((rr >> 2) & 1) + 4 * (rr >> 3) + (rr & 3);
+                const bool mine = tok >= t0 && tok < t1;
+                if (mine && s_bad[tok]) p.x[0][i][u] = make_uint4(0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u);
+                if (mine || (tok < t0 && carry)) *(uint4 *)(hot.k + at.hot + off) = p.x[0][i][u];
+                if (out && (mine || (tok < t0 && carry))) *(uint4 *)(ring.k + at.ring + off) = p.x[0][i][u];
+            }
+            const int tok0 = blk + 16 * half + 8 * (f & 1), ch = f % (HD / 16) / 2 * 32 + rr;     // eight tokens of a channel
+            const bool some = tok0 < t1 && tok0 + 8 > t0, old = tok0 < t0;
+            uint4 x = make_uint4(0u, 0u, 0u, 0u);
+            if (old && (some || whole || carry)) x = *(const uint4 *)(ring.v + older + off);
+            if (some) {
+                uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int tok = tok0 + e;
+                    const uint32_t y = tok >= t0 && tok < t1 && !s_bad[tok] ? s_v[tok * VS + ch] : tok < t0 ? (w[e >> 1] >> (16 * (e & 1))) & 0xffffu : 0u;
+                    w[e >> 1] = e & 1 ? (w[e >> 1] & 0xffffu) | y << 16 : (w[e >> 1] & 0xffff0000u) | y;
+                }
+                x = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+            if (some || (old && carry)) {
+                *(uint4 *)(hot.v + at.hot + off) = x;
+                if (out) *(uint4 *)(ring.v + at.ring + off) = x;
+            }
+            p.x[1][i][u] = x;
+        }
+    }
+    if (!whole) return;      // (the whole workgroup)
+    const int id = s.table[(size_t)b * s.max_blocks + page];
+    if ((unsigned)id >= (unsigned)s.n_pages) return;
+    const size_t pg = (size_t)id * Hkv + head;
+    kv8_quantise<HD>(p, pages + pg * (2 * KV8_PAGE * HD), scales + pg * 2, s_max);
+}
+
+// Where another kernel has put the pass's rows into the hot pages (the engine's QKV projection): pages that they complete go to the pool,
+// and with the rows in the scratch (is_long) the last two pages to the ring.  grid as above
+template <int HD>
+__global__ __launch_bounds__(256) void k_kv8_settle(Kv8State s, Kv8Hot hot, Kv8Hot ring, int is_long, uint8_t *__restrict__ pages, float *__restrict__ scales, int Hkv) {
+    using R = Kv8Regs<HD>;
+    __shared__ float s_max[2][4];
+    const int b = blockIdx.z, head = blockIdx.y, n = s.count[b];
+    if (n == 0) return;
+    const int st = s.start[b], end = st + n, first = st / KV8_PAGE, last = (end - 1) / KV8_PAGE, page = first + blockIdx.x;
+    if (page > last) return;
+    const bool whole = end >= (page + 1) * KV8_PAGE, out = is_long && page >= last - 1;
+    if (!whole && !out) return;
+    const Kv8At at = kv8_at(s, hot, ring, b, head, page, HD);
+    R p;
+#pragma unroll
+    for (int kv = 0; kv < 2; ++kv)
+#pragma unroll
+        for (int i = 0; i < R::PER; ++i) {
+            const int c = threadIdx.x + 256 * i;
+            if (R::NC % 256 && c >= R::NC) continue;
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const size_t off = ((size_t)((c >> 6) * 2 + u) * 64 + (c & 63)) * 8;
+                p.x[kv][i][u] = *(const uint4 *)((kv ? hot.v : hot.k) + at.hot + off);
+                if (out) *(uint4 *)((kv ? ring.v : ring.k) + at.ring + off) = p.x[kv][i][u];
+            }
+        }
+    if (!whole) return;
+    const int id = s.table[(size_t)b * s.max_blocks + page];
+    if ((unsigned)id >= (unsigned)s.n_pages) return;
+    const size_t pg = (size_t)id * Hkv + head;
+    kv8_quantise<HD>(p, pages + pg * (2 * KV8_PAGE * HD), scales + pg * 2, s_max);
+}
+
 // Rows as they stand in the cache (complete pages in 8 bits, else bf16) for n (sequence, position) pairs; zeros for a pair that names no
-// token.  One thread per (row, head, octet).
+// token.  One thread per (row, octet) of a head: the bytes of 16 tokens of a channel are one 16-byte vector, so that the tokens of a
+// workgroup, which mostly follow each other, find theirs in the lines that the first has fetched.  grid: x rows, y head
 template <typename DstT>
 __global__ __launch_bounds__(256) void k_kv8_read(Kv8State s, const int *__restrict__ seq, const int *__restrict__ pos, int n, Kv8Hot ring,
                                                   const uint8_t *__restrict__ pages, const float *__restrict__ scales, int Hkv, int hd,
                                                   DstT *__restrict__ k, DstT *__restrict__ v) {
-    const int octs = hd >> 3;
+    const int octs = hd >> 3, head = blockIdx.y;
     const size_t gid = (size_t)blockIdx.x * 256 + threadIdx.x;
-    if (gid >= (size_t)n * Hkv * octs) return;
-    const int oct = (int)(gid % octs), head = (int)((gid / octs) % Hkv), r = (int)(gid / ((size_t)octs * Hkv));
+    if (gid >= (size_t)n * octs) return;
+    const int oct = (int)(gid % octs), r = (int)(gid / octs);
     const int b = seq[r], ps = pos[r];
     float kf[8], vf[8];
 #pragma unroll
@@ -434,7 +493,7 @@ struct Kv8Attn {
     long long q_stride, out_stride;                // elements
     const uint4 *qhi, *qlo; uint4 *xhi, *xlo;      // fragments
     const int *q_row0;                             // fragments: attention row of a sequence's first row; null: 32 * sequence
-    float *part;
+    float *part; int *counters;                    // counters: zero between kernels
     int Hq, Hkv, G, rows, NS, rts;                 // NS key ranges; rts: tiles of 32 packed rows per sequence
     float scale_log2e, m_init;
 };
@@ -548,33 +607,78 @@ __device__ __forceinline__ void kv8_softmax(f32x16 (&sacc)[2], bool mask, int ke
     }
 }
 
+// Registers 8 hh .. + 7 of O^T tile tt of a lane's row, normalised: channels 32 tt + 8 q + 4 half .. + 3, q = 2 hh, 2 hh + 1
 template <int HD, int SRC>
-__device__ __forceinline__ void kv8_store(const Kv8Attn &a, const Kv8Row &r, const f32x16 (&o)[HD / 32], float inv, int lane) {
-    constexpr int HT = HD / 32;
+__device__ __forceinline__ void kv8_store(const Kv8Attn &a, const Kv8Row &r, int tt, int hh, const float (&o)[8], int lane) {
     const int half = lane >> 5;
-    if constexpr (SRC == KV8_FRAG) {
-        attn_write_frag<HD>(o, inv, r.row, r.head, a.Hq, lane, a.xhi, a.xlo);
-    } else if (r.row >= 0) {
 #pragma unroll
-        for (int tt = 0; tt < HT; ++tt)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const size_t at = (size_t)r.row * a.out_stride + r.head * HD + 32 * tt + 8 * q + 4 * half;
-                const float v0 = o[tt][4 * q] * inv, v1 = o[tt][4 * q + 1] * inv, v2 = o[tt][4 * q + 2] * inv, v3 = o[tt][4 * q + 3] * inv;
-                if constexpr (SRC == KV8_BF16) *(uint2 *)((uint16_t *)a.out + at) = make_uint2(f2bf2(v0, v1), f2bf2(v2, v3));
-                else *(float4 *)((float *)a.out + at) = make_float4(v0, v1, v2, v3);
+    for (int i = 0; i < 2; ++i) {
+        const int q = 2 * hh + i;
+        const float v0 = o[4 * i], v1 = o[4 * i + 1], v2 = o[4 * i + 2], v3 = o[4 * i + 3];
+        if constexpr (SRC == KV8_FRAG) {    // the partner lane holds the other half of an octet: see attn_write_frag
+            const float w0 = shx(v0, 32), w1 = shx(v1, 32), w2 = shx(v2, 32), w3 = shx(v3, 32);
+            if (i == half && r.row >= 0) {
+                const float v[8] = {half ? w0 : v0, half ? w1 : v1, half ? w2 : v2, half ? w3 : v3, half ? v0 : w0, half ? v1 : w1, half ? v2 : w2, half ? v3 : w3};
+                uint4 hi, lo;
+                pack8_split(v, hi, lo);
+                const size_t vec = (size_t)(r.row >> 5) * (a.Hq * HD / 16) * 64 + frag_vec(r.row & 31, r.head * (HD / 8) + tt * 4 + q);
+                a.xhi[vec] = hi;
+                a.xlo[vec] = lo;
             }
+        } else if (r.row >= 0) {
+            const size_t at = (size_t)r.row * a.out_stride + r.head * HD + 32 * tt + 8 * q + 4 * half;
+            if constexpr (SRC == KV8_BF16) *(uint2 *)((uint16_t *)a.out + at) = make_uint2(f2bf2(v0, v1), f2bf2(v2, v3));
+            else *(float4 *)((float *)a.out + at) = make_float4(v0, v1, v2, v3);
+        }
     }
 }
+
+// A tile's share of one key range, un-normalised, in register order (see AttnPartial): eight registers of O^T tile tt.  (Agent scope:
+// another XCD may read it in this launch.)
 template <int HD>
-__device__ __forceinline__ void kv8_store_part(const Kv8Attn &a, int b, int rt, int kvh, int split, const f32x16 (&o)[HD / 32], float m, float l, int lane) {
-    float *pp = a.part + ((size_t)((b * a.rts + rt) * a.Hkv + kvh) * a.NS + split) * AttnPartial<HD>::FLOATS;
+__device__ __forceinline__ void kv8_put(float *pp, int tt, int hh, const float (&o)[8], int lane) {
 #pragma unroll
-    for (int tt = 0; tt < HD / 32; ++tt)
+    for (int q = 0; q < 2; ++q)
+        store16_agent(pp + ((tt * 4 + 2 * hh + q) * 64 + lane) * 4, o[4 * q], o[4 * q + 1], o[4 * q + 2], o[4 * q + 3]);
+}
+// The NS shares of a tile, in order of range: eight registers of O^T tile tt, normalised.  rl: the lane's row of the tile.
+template <int HD, bool AGENT>
+__device__ __forceinline__ void kv8_sum(const float *p0, int NS, int tt, int hh, int lane, float m_init, float scale_log2e, float (&o)[8]) {
+    constexpr int PF = AttnPartial<HD>::FLOATS, CH = 8;       // CH ranges are requested together
+    const float *ml = p0 + 32 * HD + 2 * (lane & 31), *po = p0 + ((tt * 4 + 2 * hh) * 64 + lane) * 4;
+    auto get = [](const float *p) { return AGENT ? ld_agent2(p) : *(const float2 *)p; };
+    float M = m_init, L = 0.f;
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-            *(float4 *)(pp + ((tt * 4 + q) * 64 + lane) * 4) = make_float4(o[tt][4 * q], o[tt][4 * q + 1], o[tt][4 * q + 2], o[tt][4 * q + 3]);
-    if (lane < 32) *(float2 *)(pp + 32 * HD + 2 * lane) = make_float2(m, l);
+    for (int e = 0; e < 8; ++e) o[e] = 0.f;
+    for (int s0 = 0; s0 < NS; s0 += CH) {
+        float2 x[CH], v[CH][4];
+#pragma unroll
+        for (int u = 0; u < CH; ++u) x[u] = s0 + u < NS ? get(ml + (size_t)(s0 + u) * PF) : make_float2(m_init, 0.f);
+#pragma unroll
+        for (int u = 0; u < CH; ++u)
+            if (s0 + u < NS)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[u][e] = get(po + (size_t)(s0 + u) * PF + (e >> 1) * 256 + 2 * (e & 1));
+        float mn = M;
+#pragma unroll
+        for (int u = 0; u < CH; ++u) mn = fmaxf(mn, x[u].x);
+        const float f0 = __builtin_amdgcn_exp2f((M - mn) * scale_log2e);
+        M = mn;
+        L *= f0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[e] *= f0;
+#pragma unroll
+        for (int u = 0; u < CH; ++u)
+            if (s0 + u < NS) {
+                const float f = __builtin_amdgcn_exp2f((x[u].x - M) * scale_log2e);
+                L += f * x[u].y;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) { o[2 * e] += f * v[u][e].x; o[2 * e + 1] += f * v[u][e].y; }
+            }
+    }
+    const float inv = L == 0.f ? 0.f : 1.f / L;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) o[e] *= inv;
 }
 
 // Smallest and largest over the 32 rows of a tile of what they see; rows that see nothing count as none.
@@ -592,21 +696,48 @@ __device__ __forceinline__ Kv8Span kv8_span(const Kv8Row &r) {
     return s;
 }
 
-// Few packed rows (decoding): one tile of 32 per workgroup, whose four waves share the pages; a wave streams its pages straight to
-// registers.  grid: x = kv head + Hkv * key range, y tile, z sequence; 256 threads
+// Few packed rows (decoding): one tile of 32 per workgroup, whose eight waves share the pages of a key range; a wave streams its pages
+// straight to registers.  The launch is a chain of latencies where contexts are short, so a wave asks for its first page's number
+// before it knows what its rows see, and for the page before it has asked for Q; and a stream of memory where they are long: each
+// wave has half a page or more (8 KB with head_dim 128) on its way, K of the next page during the softmax, V during the next products.
+// The waves' results meet in LDS and, with several key ranges, in memory, where the last workgroup to arrive adds them up.
+// grid: x = kv head + Hkv * key range, y tile, z sequence; 512 threads
 template <int HD, int SRC>
-__global__ __launch_bounds__(256, 2) void k_kv8_attn_few(const Kv8Attn a) {
-    constexpr int KSQ = HD / 16, HT = HD / 32, N = Kv8Planes<HD, SRC>::N, KC = HD / 32;   // KC chunks per 32 keys of K, and of V
+__global__ __launch_bounds__(512, 1) void k_kv8_attn_few(const Kv8Attn a) {
+    constexpr int KSQ = HD / 16, HT = HD / 32, N = Kv8Planes<HD, SRC>::N, KC = HD / 32, W = 8;   // KC chunks per 32 keys of K, and of V
     __shared__ float s_o[4][HT * 16][64];
-    __shared__ float s_ml[4][2][32];
+    __shared__ float s_ml[W][2][32];
+    __shared__ int s_flag;
     const int tidx = opaque_tid();
     const int w = __builtin_amdgcn_readfirstlane(tidx >> 6), lane = tidx & 63, half = lane >> 5;
     const int b = blockIdx.z, rt = blockIdx.y, kvh = blockIdx.x % opaque_s(a.Hkv), split = blockIdx.x / opaque_s(a.Hkv);
+    const int stride = W * a.NS, *table = a.s.table + (size_t)b * a.s.max_blocks;
+    int u = split * W + w;
+    auto page_of = [&](int i) { return __builtin_amdgcn_readfirstlane(table[min(i, a.s.max_blocks - 1)]); };
+    auto valid = [&](int id) { return (unsigned)id < (unsigned)a.s.n_pages; };
+    auto base_of = [&](int i) { return (size_t)(valid(i) ? i : 0) * a.Hkv + kvh; };   // (a page that does not exist is read as page 0 and masked)
+    uint4 kc[2 * KC], vc[2 * KC];
+    float ks1, vs1;
+    auto load_k = [&](int i) {
+        const uint4 *p = (const uint4 *)(a.pages + base_of(i) * (2 * KV8_PAGE * HD)) + lane;
+#pragma unroll
+        for (int c = 0; c < 2 * KC; ++c) kc[c] = p[c * 64];
+        ks1 = a.scales[base_of(i) * 2];
+    };
+    auto load_v = [&](int i) {
+        const uint4 *p = (const uint4 *)(a.pages + base_of(i) * (2 * KV8_PAGE * HD) + KV8_PAGE * HD) + lane;
+#pragma unroll
+        for (int c = 0; c < 2 * KC; ++c) vc[c] = p[c * 64];
+        vs1 = a.scales[base_of(i) * 2 + 1];
+    };
+    int id = page_of(u), id1 = page_of(u + stride);
     if (rt * 32 >= (a.s.cu[b + 1] - a.s.cu[b]) * a.G) return;
+    load_k(id);
     const Kv8Row r = kv8_row(a, b, kvh, rt * 32 + (lane & 31));
-    const Kv8Span sp = kv8_span(r);
     uint4 q[N][KSQ];
     kv8_load_q<HD, SRC>(a, r, b, half, q);
+    load_v(id);
+    const Kv8Span sp = kv8_span(r);
     f32x16 oacc[HT];
 #pragma unroll
     for (int tt = 0; tt < HT; ++tt)
@@ -644,50 +775,25 @@ __global__ __launch_bounds__(256, 2) void k_kv8_attn_few(const Kv8Attn a) {
                 }
         }
     };
-    const int n8 = (sp.max8 + KV8_PAGE - 1) / KV8_PAGE, nh = max(0, sp.hmax - sp.hmin + 1), stride = 4 * a.NS;
-    int u = split * 4 + w;
-    const int *table = a.s.table + (size_t)b * a.s.max_blocks;
-    auto page_of = [&](int i) { return __builtin_amdgcn_readfirstlane(i < n8 ? table[i] : -1); };
-    auto valid = [&](int id) { return (unsigned)id < (unsigned)a.s.n_pages; };
-    if (u < n8) {
-        uint4 kc[2 * KC], vc[2 * KC];
-        float ks, vs, ks1, vs1;
-        int id = page_of(u);
-        bool live = valid(id);
-        auto base_of = [&](int i) { return (size_t)(valid(i) ? i : 0) * a.Hkv + kvh; };   // (a page that does not exist is read as page 0 and masked)
-        auto load_k = [&](int i) {
-            const uint4 *p = (const uint4 *)(a.pages + base_of(i) * (2 * KV8_PAGE * HD)) + lane;
-#pragma unroll
-            for (int c = 0; c < 2 * KC; ++c) kc[c] = p[c * 64];
-            ks1 = a.scales[base_of(i) * 2];
-        };
-        auto load_v = [&](int i) {
-            const uint4 *p = (const uint4 *)(a.pages + base_of(i) * (2 * KV8_PAGE * HD) + KV8_PAGE * HD) + lane;
-#pragma unroll
-            for (int c = 0; c < 2 * KC; ++c) vc[c] = p[c * 64];
-            vs1 = a.scales[base_of(i) * 2 + 1];
-        };
-        load_k(id);
-        load_v(id);
-        int id1 = page_of(u + stride);
-        for (; u < n8; u += stride) {
-            const int id2 = page_of(u + 2 * stride);
-            ks = ks1; vs = vs1;
-            f32x16 sacc[2];
-            scores(sacc, [&](int j, int s) {
-                const uint4 c = kc[j * KC + (s >> 1)];
-                return s & 1 ? dequant8(c.z, c.w, ks) : dequant8(c.x, c.y, ks);
-            });
-            if (u + stride < n8) load_k(id1);
-            const int key0 = u * KV8_PAGE + 16 * half;
-            kv8_softmax<HT>(sacc, (u + 1) * KV8_PAGE > sp.min8 || !live, key0, 0, live ? r.lim8 : 0, a.scale_log2e, m_run, l_run, oacc);
-            values(sacc, [&](int j, int tt, int s2) {
-                const uint4 c = vc[j * KC + tt];
-                return s2 ? dequant8(c.z, c.w, vs) : dequant8(c.x, c.y, vs);
-            });
-            if (u + stride < n8) load_v(id1);
-            id = id1; live = valid(id1); id1 = id2;
-        }
+    const int n8 = (sp.max8 + KV8_PAGE - 1) / KV8_PAGE, nh = max(0, sp.hmax - sp.hmin + 1);
+    for (; u < n8; u += stride) {
+        const int id2 = page_of(u + 2 * stride);
+        const bool live = valid(id);
+        const float ks = ks1, vs = vs1;
+        f32x16 sacc[2];
+        scores(sacc, [&](int j, int s) {
+            const uint4 c = kc[j * KC + (s >> 1)];
+            return s & 1 ? dequant8(c.z, c.w, ks) : dequant8(c.x, c.y, ks);
+        });
+        if (u + stride < n8) load_k(id1);
+        const int key0 = u * KV8_PAGE + 16 * half;
+        kv8_softmax<HT>(sacc, (u + 1) * KV8_PAGE > sp.min8 || !live, key0, 0, live ? r.lim8 : 0, a.scale_log2e, m_run, l_run, oacc);
+        values(sacc, [&](int j, int tt, int s2) {
+            const uint4 c = vc[j * KC + tt];
+            return s2 ? dequant8(c.z, c.w, vs) : dequant8(c.x, c.y, vs);
+        });
+        if (u + stride < n8) load_v(id1);
+        id = id1; id1 = id2;
     }
     for (; u < n8 + nh; u += stride) {       // hot pages
         const int page = sp.hmin + u - n8;
@@ -699,29 +805,49 @@ __global__ __launch_bounds__(256, 2) void k_kv8_attn_few(const Kv8Attn a) {
         kv8_softmax<HT>(sacc, true, page * KV8_PAGE + 16 * half, 0, own ? r.lim : 0, a.scale_log2e, m_run, l_run, oacc);
         values(sacc, [&](int j, int tt, int s2) { return vp[(j * KSQ + tt * 2 + s2) * 64]; });
     }
-    // the four waves' shares meet: all to LDS, wave w sums O^T tile w (of up to four)
+    // the waves' shares: waves 4 .. 7 hand theirs to waves 0 .. 3, then every wave adds up eight registers of a tile
     const float l_tot = l_run + shx(l_run, 32);
     if (lane < 32) { s_ml[w][0][lane] = m_run; s_ml[w][1][lane] = l_tot; }
     __syncthreads();
-    float M = s_ml[0][0][lane & 31];
+    float M = a.m_init, L = 0.f;
 #pragma unroll
-    for (int i = 1; i < 4; ++i) M = fmaxf(M, s_ml[i][0][lane & 31]);
+    for (int i = 0; i < W; ++i) M = fmaxf(M, s_ml[i][0][lane & 31]);
+#pragma unroll
+    for (int i = 0; i < W; ++i) L += s_ml[i][1][lane & 31] * __builtin_amdgcn_exp2f((s_ml[i][0][lane & 31] - M) * a.scale_log2e);
     const float f = __builtin_amdgcn_exp2f((m_run - M) * a.scale_log2e);
+    if (w >= 4)
 #pragma unroll
-    for (int tt = 0; tt < HT; ++tt)
+        for (int tt = 0; tt < HT; ++tt)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) s_o[w][tt * 16 + e][lane] = oacc[tt][e] * f;
-    float L = 0.f;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) L += s_ml[i][1][lane & 31] * __builtin_amdgcn_exp2f((s_ml[i][0][lane & 31] - M) * a.scale_log2e);
+            for (int e = 0; e < 16; ++e) s_o[w - 4][tt * 16 + e][lane] = oacc[tt][e] * f;
     __syncthreads();
-    if (w > 0) return;
+    if (w < 4)
 #pragma unroll
-    for (int tt = 0; tt < HT; ++tt)
+        for (int tt = 0; tt < HT; ++tt)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) oacc[tt][e] = (s_o[0][tt * 16 + e][lane] + s_o[1][tt * 16 + e][lane]) + (s_o[2][tt * 16 + e][lane] + s_o[3][tt * 16 + e][lane]);
-    if (a.NS == 1) kv8_store<HD, SRC>(a, r, oacc, L == 0.f ? 0.f : 1.f / L, lane);
-    else kv8_store_part<HD>(a, b, rt, kvh, split, oacc, M, L, lane);
+            for (int e = 0; e < 16; ++e) s_o[w][tt * 16 + e][lane] += oacc[tt][e] * f;
+    __syncthreads();
+    const int tt = w >> 1, hh = w & 1;
+    const bool on = tt < HT;
+    float o[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const int i = min(tt, HT - 1) * 16 + 8 * hh + e;
+        o[e] = (s_o[0][i][lane] + s_o[1][i][lane]) + (s_o[2][i][lane] + s_o[3][i][lane]);
+    }
+    if (a.NS > 1) {
+        const size_t item = (size_t)(b * a.rts + rt) * a.Hkv + kvh;
+        float *p0 = a.part + item * a.NS * AttnPartial<HD>::FLOATS, *pp = p0 + (size_t)split * AttnPartial<HD>::FLOATS;
+        if (on && r.row >= 0) kv8_put<HD>(pp, tt, hh, o, lane);
+        if (w == 0 && lane < 32 && r.row >= 0) st_agent2(pp + 32 * HD + 2 * lane, M, L);
+        if (!arrive_last(a.counters + item, a.NS, &s_flag) || !on) return;
+        if (r.row >= 0) kv8_sum<HD, true>(p0, a.NS, tt, hh, lane, a.m_init, a.scale_log2e, o);
+    } else {
+        const float inv = L == 0.f ? 0.f : 1.f / L;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[e] *= inv;
+    }
+    if (on) kv8_store<HD, SRC>(a, r, tt, hh, o, lane);
 }
 
 // Many packed rows (blocks of a group, prompts): four tiles of 32 per workgroup, one per wave; a page is made bf16 once by all four, in
@@ -729,7 +855,7 @@ __global__ __launch_bounds__(256, 2) void k_kv8_attn_few(const Kv8Attn a) {
 // under the products of page i.  grid: x = kv head + Hkv * key range, y group of four tiles counted from the last (prompts: the
 // longest start first), z sequence; 256 threads
 template <int HD, int SRC>
-__global__ __launch_bounds__(256, 2) void k_kv8_attn_many(const Kv8Attn a) {
+__global__ __launch_bounds__(256, HD == 128 && SRC == KV8_F32 ? 1 : 2) void k_kv8_attn_many(const Kv8Attn a) {
     constexpr int KSQ = HD / 16, HT = HD / 32, N = Kv8Planes<HD, SRC>::N, FR = HD / 8;    // FR fragments of 1 KB of K, and of V, per page
     constexpr int LPW = HD / 32;           // chunks per wave and page; of the HD / 8 chunks the first half is K
     __shared__ __attribute__((aligned(16))) uint4 buf[2][2 * FR * 64];
@@ -839,39 +965,34 @@ __global__ __launch_bounds__(256, 2) void k_kv8_attn_many(const Kv8Attn a) {
         }
     }
     if (!active) return;
-    const float l_tot = l_run + shx(l_run, 32);
-    if (a.NS == 1) kv8_store<HD, SRC>(a, r, oacc, l_tot == 0.f ? 0.f : 1.f / l_tot, lane);
-    else kv8_store_part<HD>(a, b, rt, kvh, split, oacc, m_run, l_tot, lane);
-}
-
-// The key ranges of a tile meet, in order.  grid: x kv head, y tile, z sequence; 64 threads
-template <int HD, int SRC>
-__global__ __launch_bounds__(64) void k_kv8_merge(const Kv8Attn a) {
-    constexpr int HT = HD / 32, PF = AttnPartial<HD>::FLOATS;
-    const int lane = threadIdx.x, b = blockIdx.z, rt = blockIdx.y, kvh = blockIdx.x;
-    if (rt * 32 >= (a.s.cu[b + 1] - a.s.cu[b]) * a.G) return;
-    const Kv8Row r = kv8_row(a, b, kvh, rt * 32 + (lane & 31));
-    const float *p0 = a.part + (size_t)((b * a.rts + rt) * a.Hkv + kvh) * a.NS * PF;
-    float M = a.m_init, L = 0.f;
-    for (int s = 0; s < a.NS; ++s) M = fmaxf(M, p0[(size_t)s * PF + 32 * HD + 2 * (lane & 31)]);
-    f32x16 o[HT];
+    const float l_tot = l_run + shx(l_run, 32), inv = a.NS > 1 ? 1.f : l_tot == 0.f ? 0.f : 1.f / l_tot;
+    float *pp = a.part + ((size_t)((b * a.rts + rt) * a.Hkv + kvh) * a.NS + split) * AttnPartial<HD>::FLOATS;
+    if (a.NS > 1 && lane < 32) *(float2 *)(pp + 32 * HD + 2 * lane) = make_float2(m_run, l_tot);
 #pragma unroll
     for (int tt = 0; tt < HT; ++tt)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) o[tt][e] = 0.f;
-    for (int s = 0; s < a.NS; ++s) {
-        const float2 ml = *(const float2 *)(p0 + (size_t)s * PF + 32 * HD + 2 * (lane & 31));
-        const float f = __builtin_amdgcn_exp2f((ml.x - M) * a.scale_log2e);
-        L += f * ml.y;
+        for (int hh = 0; hh < 2; ++hh) {
+            float o[8];
 #pragma unroll
-        for (int tt = 0; tt < HT; ++tt)
+            for (int e = 0; e < 8; ++e) o[e] = oacc[tt][8 * hh + e] * inv;
+            if (a.NS == 1) kv8_store<HD, SRC>(a, r, tt, hh, o, lane);
+            else
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const float4 v = *(const float4 *)(p0 + (size_t)s * PF + ((tt * 4 + q) * 64 + lane) * 4);
-                o[tt][4 * q] += f * v.x; o[tt][4 * q + 1] += f * v.y; o[tt][4 * q + 2] += f * v.z; o[tt][4 * q + 3] += f * v.w;
-            }
-    }
-    kv8_store<HD, SRC>(a, r, o, L == 0.f ? 0.f : 1.f / L, lane);
+                for (int q = 0; q < 2; ++q) *(float4 *)(pp + ((tt * 4 + 2 * hh + q) * 64 + lane) * 4) = make_float4(o[4 * q], o[4 * q + 1], o[4 * q + 2], o[4 * q + 3]);
+        }
+}
+
+// The key ranges of k_kv8_attn_many's tiles meet, one wave per eight registers of an O^T tile (in the launch itself the last workgroup
+// to arrive would read all of four tiles' shares alone: 44 us for 8 heads, 32 rows and 16 ranges, 15 + 4 so).
+// grid: x kv head, y tile, z sequence; 64 * HD / 16 threads
+template <int HD, int SRC>
+__global__ __launch_bounds__(512) void k_kv8_merge(const Kv8Attn a) {
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, b = blockIdx.z, rt = blockIdx.y, kvh = blockIdx.x;
+    if (rt * 32 >= (a.s.cu[b + 1] - a.s.cu[b]) * a.G) return;
+    const Kv8Row r = kv8_row(a, b, kvh, rt * 32 + (lane & 31));
+    float o[8];
+    kv8_sum<HD, false>(a.part + (size_t)((b * a.rts + rt) * a.Hkv + kvh) * a.NS * AttnPartial<HD>::FLOATS, a.NS, w >> 1, w & 1, lane, a.m_init, a.scale_log2e, o);
+    kv8_store<HD, SRC>(a, r, w >> 1, w & 1, o, lane);
 }
 
 }  // namespace deer

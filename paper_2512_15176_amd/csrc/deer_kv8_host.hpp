@@ -19,6 +19,7 @@ struct Kv8Cache {
     Kv8State st{};
     uint8_t *pages = nullptr;
     float *scales = nullptr, *part = nullptr;
+    int *counters = nullptr;
     uint16_t *ring = nullptr, *scratch = nullptr;
     int *ask_start = nullptr, *ask_count = nullptr, *ask_row0 = nullptr;   // requests that the library makes up itself, [max_batch]
     size_t scratch_slots = 0, cache_bytes = 0, work_bytes = 0;
@@ -78,6 +79,7 @@ inline void plan_kv8(Kv8Cache &c, const Kv8Shape &p, char *cache, char *work) {
     // a sequence's rows of a long pass touch whole pages: up to 127 slots more than rows
     c.scratch_slots = p.max_rows > KV8_PAGE ? ((size_t)p.max_rows + (size_t)std::min(p.max_batch, p.max_rows) * 127 + 63) / 64 * 64 : 0;
     c.scratch = (uint16_t *)take(2 * c.scratch_slots * p.n_kv_heads * p.head_dim * 2);
+    c.counters = (int *)take(KV8_PART_TILES * 4);      // of the items whose key ranges meet: no more than tiles
     c.part = (float *)take((size_t)KV8_PART_TILES * (32 * p.head_dim + 64) * 4);
     c.work_bytes = off;
 }
@@ -85,7 +87,7 @@ inline void plan_kv8(Kv8Cache &c, const Kv8Shape &p, char *cache, char *work) {
 // everything finite, no tokens (masked keys are multiplied by zero weights)
 inline hipError_t kv8_clear(Kv8Cache &c, hipStream_t s) {
     hipError_t e = hipMemsetAsync(c.pages, 0, (char *)c.st.table - (char *)c.pages, s);
-    if (e == hipSuccess && c.scratch_slots) e = hipMemsetAsync(c.scratch, 0, (char *)c.part - (char *)c.scratch, s);
+    if (e == hipSuccess) e = hipMemsetAsync(c.scratch, 0, (char *)c.part - (char *)c.scratch, s);   // and the counters
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(k_kv8_init, dim3(256), dim3(256), 0, s, c.st);
     c.batch = c.rows = 0;
@@ -111,10 +113,12 @@ inline hipError_t kv8_reserve(Kv8Cache &c, hipStream_t s, const int *start, int 
     return hipGetLastError();
 }
 
+// pages that a sequence of the pass may touch
+inline unsigned kv8_touched(const Kv8Cache &c) { return (unsigned)(c.max_new + KV8_PAGE - 2) / KV8_PAGE + 1; }
+
 template <int HD>
 hipError_t kv8_settle_hd(Kv8Cache &c, hipStream_t s, int layer) {
-    const Kv8Hot ring = c.long_pass ? c.ring_view(layer) : Kv8Hot{};
-    hipLaunchKernelGGL(k_kv8_settle<HD>, dim3((c.max_new + KV8_PAGE - 2) / KV8_PAGE + 1, c.p.n_kv_heads, c.batch), dim3(256), 0, s, c.st, c.hot_view(layer), ring,
+    hipLaunchKernelGGL(k_kv8_settle<HD>, dim3(kv8_touched(c), c.p.n_kv_heads, c.batch), dim3(256), 0, s, c.st, c.hot_view(layer), c.ring_view(layer), c.long_pass ? 1 : 0,
                        c.layer_pages(layer), c.layer_scales(layer), c.p.n_kv_heads);
     return hipGetLastError();
 }
@@ -124,15 +128,22 @@ inline hipError_t kv8_settle(Kv8Cache &c, hipStream_t s, int layer) {
     return c.p.head_dim == 128 ? kv8_settle_hd<128>(c, s, layer) : c.p.head_dim == 64 ? kv8_settle_hd<64>(c, s, layer) : kv8_settle_hd<32>(c, s, layer);
 }
 
-template <typename T>
-hipError_t kv8_write(Kv8Cache &c, hipStream_t s, int layer, const T *k, const T *v, size_t k_stride, size_t v_stride) {
-    const Kv8Shape &p = c.p;
-    if (c.rows == 0) return hipSuccess;
-    const size_t items = (size_t)c.rows * p.n_kv_heads * (p.head_dim / 8);
-    const unsigned row_wgs = (unsigned)((items + 255) / 256);
-    hipLaunchKernelGGL(k_kv8_write<T>, dim3(row_wgs + c.batch * p.n_kv_heads), dim3(256), 0, s, c.st, k, v, k_stride, v_stride, c.hot_view(layer), c.ring_view(layer),
-                       c.rows, (int)row_wgs, p.n_kv_heads, p.head_dim);
+template <int HD, typename T>
+hipError_t kv8_append_hd(Kv8Cache &c, hipStream_t s, int layer, const T *k, const T *v, size_t k_stride, size_t v_stride) {
+    const Kv8Hot ring = c.ring_view(layer);
+    if (c.long_pass) {
+        hipLaunchKernelGGL(k_kv8_keep<HD>, dim3(c.p.n_kv_heads, c.batch), dim3(256), 0, s, c.st, ring);
+        if (hipError_t e = hipGetLastError()) return e;
+    }
+    hipLaunchKernelGGL((k_kv8_append<HD, T>), dim3(kv8_touched(c), c.p.n_kv_heads, c.batch), dim3(256), 0, s, c.st, k, v, k_stride, v_stride, c.hot_view(layer), ring,
+                       c.long_pass ? 1 : 0, c.layer_pages(layer), c.layer_scales(layer), c.p.n_kv_heads);
     return hipGetLastError();
+}
+template <typename T>
+hipError_t kv8_append(Kv8Cache &c, hipStream_t s, int layer, const T *k, const T *v, size_t k_stride, size_t v_stride) {
+    if (c.rows == 0 || c.max_new == 0) return hipSuccess;
+    return c.p.head_dim == 128 ? kv8_append_hd<128>(c, s, layer, k, v, k_stride, v_stride)
+           : c.p.head_dim == 64 ? kv8_append_hd<64>(c, s, layer, k, v, k_stride, v_stride) : kv8_append_hd<32>(c, s, layer, k, v, k_stride, v_stride);
 }
 
 template <int HD, int SRC>
@@ -142,13 +153,14 @@ hipError_t kv8_attend_src(Kv8Cache &c, hipStream_t s, Kv8Attn &a) {
     const bool few = packed <= 32;
     const int ty = few ? a.rts : (a.rts + 3) / 4;
     const long long items = (long long)B * ty * a.Hkv, tiles = (long long)B * a.rts * a.Hkv;
-    // key ranges: as many as fill the chip, each with work for all of its waves
-    a.NS = (int)std::max<long long>(1, std::min<long long>({KV8_WGS / std::max<long long>(items, 1), KV8_PART_TILES / tiles, 64, std::max(1, pages / 4)}));
+    // key ranges: as many as fill the chip (one workgroup of eight waves per compute unit, or two of four), each with work for its waves
+    const long long fill = (few ? KV8_WGS / 2 : KV8_WGS) / std::max<long long>(items, 1);
+    a.NS = (int)std::max<long long>(1, std::min<long long>({fill, KV8_PART_TILES / tiles, 64, few ? (pages + 7) / 8 : std::max(1, pages / 4)}));
     const dim3 grid(a.Hkv * a.NS, ty, B);
-    if (few) hipLaunchKernelGGL((k_kv8_attn_few<HD, SRC>), grid, dim3(256), 0, s, a);
+    if (few) hipLaunchKernelGGL((k_kv8_attn_few<HD, SRC>), grid, dim3(512), 0, s, a);
     else hipLaunchKernelGGL((k_kv8_attn_many<HD, SRC>), grid, dim3(256), 0, s, a);
     if (hipError_t e = hipGetLastError()) return e;
-    if (a.NS > 1) hipLaunchKernelGGL((k_kv8_merge<HD, SRC>), dim3(a.Hkv, a.rts, B), dim3(64), 0, s, a);
+    if (!few && a.NS > 1) hipLaunchKernelGGL((k_kv8_merge<HD, SRC>), dim3(a.Hkv, a.rts, B), dim3(4 * HD), 0, s, a);
     return hipGetLastError();
 }
 // a: what the caller knows (limits, q, out or fragments)
@@ -156,7 +168,7 @@ template <int SRC>
 hipError_t kv8_attend(Kv8Cache &c, hipStream_t s, int layer, Kv8Attn a, double scale) {
     if (c.rows == 0 || c.max_new == 0) return hipSuccess;
     a.s = c.st; a.hot = c.hot_view(layer); a.pages = c.layer_pages(layer); a.scales = c.layer_scales(layer);
-    a.part = c.part; a.Hq = c.p.n_q_heads; a.Hkv = c.p.n_kv_heads; a.G = a.Hq / a.Hkv; a.rows = c.rows;
+    a.part = c.part; a.counters = c.counters; a.Hq = c.p.n_q_heads; a.Hkv = c.p.n_kv_heads; a.G = a.Hq / a.Hkv; a.rows = c.rows;
     a.scale_log2e = (float)(scale * 1.4426950408889634);
     a.m_init = -3e38f / std::max(1.f, a.scale_log2e);     // times scale_log2e it stays finite
     return c.p.head_dim == 128 ? kv8_attend_src<128, SRC>(c, s, a) : c.p.head_dim == 64 ? kv8_attend_src<64, SRC>(c, s, a) : kv8_attend_src<32, SRC>(c, s, a);
