@@ -544,67 +544,78 @@ __device__ __forceinline__ Kv8Row kv8_row(const Kv8Attn &a, int b, int kvh, int 
 template <int HD, int SRC>
 struct Kv8Planes { static constexpr int N = SRC == KV8_BF16 ? 1 : SRC == KV8_F32 ? 3 : 2; };
 
+// q elements e0 .. e0 + 7 of a lane's row, as planes
+template <int HD, int SRC>
+__device__ __forceinline__ void kv8_q8(const Kv8Attn &a, const Kv8Row &r, int b, int e0, uint4 (&o)[Kv8Planes<HD, SRC>::N]) {
+    const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+    if constexpr (SRC == KV8_BF16) {
+        o[0] = r.row < 0 ? zero : *(const uint4 *)((const uint16_t *)a.q + (size_t)r.row * a.q_stride + r.head * HD + e0);
+    } else if constexpr (SRC == KV8_F32) {
+        float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (r.row >= 0) {
+            const float4 *p = (const float4 *)((const float *)a.q + (size_t)r.row * a.q_stride + r.head * HD + e0);
+            const float4 x = p[0], y = p[1];
+            v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w; v[4] = y.x; v[5] = y.y; v[6] = y.z; v[7] = y.w;
+        }
+        split_planes<3>(v, o);
+    } else {
+        const int ar = r.row < 0 ? 0 : (a.q_row0 ? a.q_row0[b] : 32 * b) + r.row - a.s.cu[b];
+        const size_t vec = ((size_t)((ar >> 5) * a.Hq + r.head) * (HD / 16)) * 64 + frag_vec(ar & 31, e0 >> 3);
+        o[0] = r.row < 0 ? zero : a.qhi[vec];
+        o[1] = r.row < 0 ? zero : a.qlo[vec];
+    }
+}
 // Q fragments of a tile: [plane][k-step]
 template <int HD, int SRC>
 __device__ __forceinline__ void kv8_load_q(const Kv8Attn &a, const Kv8Row &r, int b, int half, uint4 (&q)[Kv8Planes<HD, SRC>::N][HD / 16]) {
     constexpr int KSQ = HD / 16;
-    const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
     for (int s = 0; s < KSQ; ++s) {
-        if constexpr (SRC == KV8_BF16) {
-            q[0][s] = r.row < 0 ? zero : *(const uint4 *)((const uint16_t *)a.q + (size_t)r.row * a.q_stride + r.head * HD + 16 * s + 8 * half);
-        } else if constexpr (SRC == KV8_F32) {
-            float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-            if (r.row >= 0) {
-                const float4 *p = (const float4 *)((const float *)a.q + (size_t)r.row * a.q_stride + r.head * HD + 16 * s + 8 * half);
-                const float4 x = p[0], y = p[1];
-                v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w; v[4] = y.x; v[5] = y.y; v[6] = y.z; v[7] = y.w;
-            }
-            uint4 pl[3];
-            split_planes<3>(v, pl);
-            q[0][s] = pl[0]; q[1][s] = pl[1]; q[2][s] = pl[2];
-        } else {
-            const int ar = r.row < 0 ? 0 : (a.q_row0 ? a.q_row0[b] : 32 * b) + r.row - a.s.cu[b];
-            const size_t vec = ((size_t)((ar >> 5) * a.Hq + r.head) * KSQ + s) * 64 + half * 32 + (ar & 31);
-            q[0][s] = r.row < 0 ? zero : a.qhi[vec];
-            q[1][s] = r.row < 0 ? zero : a.qlo[vec];
-        }
+        uint4 o[Kv8Planes<HD, SRC>::N];
+        kv8_q8<HD, SRC>(a, r, b, 16 * s + 8 * half, o);
+#pragma unroll
+        for (int p = 0; p < Kv8Planes<HD, SRC>::N; ++p) q[p][s] = o[p];
     }
 }
 
 // One step over 64 keys: scores (raw, of two tiles of 32 keys; the lane's keys are key0 + r and key0 + 32 + r) to weights, running
-// maximum and sum, rescaled result.
+// reference and sum, rescaled result.  First the reference: the largest score when it was last moved.  It moves where a score is more than
+// 2^8 weights above it, not with every new maximum (of 32 rows one has a new maximum on almost every page of the first few thousand
+// keys): weights are then at most 2^8, as exact relative to each other as before.
+constexpr float KV8_SLACK = 8.f;      // log2 of the largest weight
 template <int HT>
-__device__ __forceinline__ void kv8_softmax(f32x16 (&sacc)[2], bool mask, int key0, int lo, int hi, float scale_log2e, float &m_run,
-                                            float &l_run, f32x16 (&oacc)[HT]) {
+__device__ __forceinline__ void kv8_rescale(f32x16 (&sacc)[2], bool mask, int key0, int hi, float scale_log2e, float &m_run, float &l_run, f32x16 (&oacc)[HT]) {
     if (mask) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-            if (key0 + r >= hi || key0 + r < lo) sacc[0][r] = -INFINITY;
-            if (key0 + 32 + r >= hi || key0 + 32 + r < lo) sacc[1][r] = -INFINITY;
+            if (key0 + r >= hi) sacc[0][r] = -INFINITY;
+            if (key0 + 32 + r >= hi) sacc[1][r] = -INFINITY;
         }
     }
     float mx = fmaxf(sacc[0][0], sacc[1][0]);
 #pragma unroll
     for (int r = 1; r < 16; ++r) mx = fmaxf(mx, fmaxf(sacc[0][r], sacc[1][r]));
-    mx = fmaxf(mx, shx(mx, 32));
-    const float m_new = fmaxf(m_run, mx);
-    const float alpha = __builtin_amdgcn_exp2f((m_run - m_new) * scale_log2e);
-    const float mb = m_new * scale_log2e;
-    float ls0 = 0.f, ls1 = 0.f;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-        sacc[0][r] = __builtin_amdgcn_exp2f(sacc[0][r] * scale_log2e - mb); ls0 += sacc[0][r];
-        sacc[1][r] = __builtin_amdgcn_exp2f(sacc[1][r] * scale_log2e - mb); ls1 += sacc[1][r];
-    }
-    l_run = l_run * alpha + (ls0 + ls1);
-    m_run = m_new;
-    if (__builtin_amdgcn_ballot_w64(alpha != 1.f)) {
+    if (__builtin_amdgcn_ballot_w64((mx - m_run) * scale_log2e > KV8_SLACK)) {
+        const float m_new = fmaxf(m_run, fmaxf(mx, shx(mx, 32)));
+        const float alpha = __builtin_amdgcn_exp2f((m_run - m_new) * scale_log2e);
+        m_run = m_new;
+        l_run *= alpha;
 #pragma unroll
         for (int tt = 0; tt < HT; ++tt)
 #pragma unroll
             for (int r = 0; r < 16; ++r) oacc[tt][r] *= alpha;
     }
+}
+// .. then the weights.
+__device__ __forceinline__ void kv8_weights(f32x16 (&sacc)[2], float scale_log2e, float m_run, float &l_run) {
+    const float mb = m_run * scale_log2e;
+    float ls0 = 0.f, ls1 = 0.f;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+        sacc[0][r] = __builtin_amdgcn_exp2f(fmaf(sacc[0][r], scale_log2e, -mb)); ls0 += sacc[0][r];
+        sacc[1][r] = __builtin_amdgcn_exp2f(fmaf(sacc[1][r], scale_log2e, -mb)); ls1 += sacc[1][r];
+    }
+    l_run += ls0 + ls1;
 }
 
 // Registers 8 hh .. + 7 of O^T tile tt of a lane's row, normalised: channels 32 tt + 8 q + 4 half .. + 3, q = 2 hh, 2 hh + 1
@@ -614,7 +625,8 @@ __device__ __forceinline__ void kv8_store(const Kv8Attn &a, const Kv8Row &r, int
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         const int q = 2 * hh + i;
-        const float v0 = o[4 * i], v1 = o[4 * i + 1], v2 = o[4 * i + 2], v3 = o[4 * i + 3];
+        // (a row that sees nothing is not masked where the others of its tile need no mask)
+        const float v0 = r.lim > 0 ? o[4 * i] : 0.f, v1 = r.lim > 0 ? o[4 * i + 1] : 0.f, v2 = r.lim > 0 ? o[4 * i + 2] : 0.f, v3 = r.lim > 0 ? o[4 * i + 3] : 0.f;
         if constexpr (SRC == KV8_FRAG) {    // the partner lane holds the other half of an octet: see attn_write_frag
             const float w0 = shx(v0, 32), w1 = shx(v1, 32), w2 = shx(v2, 32), w3 = shx(v3, 32);
             if (i == half && r.row >= 0) {
@@ -633,32 +645,24 @@ __device__ __forceinline__ void kv8_store(const Kv8Attn &a, const Kv8Row &r, int
     }
 }
 
-// A tile's share of one key range, un-normalised, in register order (see AttnPartial): eight registers of O^T tile tt.  (Agent scope:
-// another XCD may read it in this launch.)
-template <int HD>
-__device__ __forceinline__ void kv8_put(float *pp, int tt, int hh, const float (&o)[8], int lane) {
-#pragma unroll
-    for (int q = 0; q < 2; ++q)
-        store16_agent(pp + ((tt * 4 + 2 * hh + q) * 64 + lane) * 4, o[4 * q], o[4 * q + 1], o[4 * q + 2], o[4 * q + 3]);
-}
 // The NS shares of a tile, in order of range: eight registers of O^T tile tt, normalised.  rl: the lane's row of the tile.
-template <int HD, bool AGENT>
+template <int HD>
 __device__ __forceinline__ void kv8_sum(const float *p0, int NS, int tt, int hh, int lane, float m_init, float scale_log2e, float (&o)[8]) {
     constexpr int PF = AttnPartial<HD>::FLOATS, CH = 8;       // CH ranges are requested together
     const float *ml = p0 + 32 * HD + 2 * (lane & 31), *po = p0 + ((tt * 4 + 2 * hh) * 64 + lane) * 4;
-    auto get = [](const float *p) { return AGENT ? ld_agent2(p) : *(const float2 *)p; };
     float M = m_init, L = 0.f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) o[e] = 0.f;
     for (int s0 = 0; s0 < NS; s0 += CH) {
-        float2 x[CH], v[CH][4];
+        float2 x[CH];
+        float4 v[CH][2];
 #pragma unroll
-        for (int u = 0; u < CH; ++u) x[u] = s0 + u < NS ? get(ml + (size_t)(s0 + u) * PF) : make_float2(m_init, 0.f);
+        for (int u = 0; u < CH; ++u) x[u] = s0 + u < NS ? *(const float2 *)(ml + (size_t)(s0 + u) * PF) : make_float2(m_init, 0.f);
 #pragma unroll
         for (int u = 0; u < CH; ++u)
             if (s0 + u < NS)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[u][e] = get(po + (size_t)(s0 + u) * PF + (e >> 1) * 256 + 2 * (e & 1));
+                for (int e = 0; e < 2; ++e) v[u][e] = *(const float4 *)(po + (size_t)(s0 + u) * PF + e * 256);
         float mn = M;
 #pragma unroll
         for (int u = 0; u < CH; ++u) mn = fmaxf(mn, x[u].x);
@@ -673,7 +677,7 @@ __device__ __forceinline__ void kv8_sum(const float *p0, int NS, int tt, int hh,
                 const float f = __builtin_amdgcn_exp2f((x[u].x - M) * scale_log2e);
                 L += f * x[u].y;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) { o[2 * e] += f * v[u][e].x; o[2 * e + 1] += f * v[u][e].y; }
+                for (int e = 0; e < 2; ++e) { o[4 * e] += f * v[u][e].x; o[4 * e + 1] += f * v[u][e].y; o[4 * e + 2] += f * v[u][e].z; o[4 * e + 3] += f * v[u][e].w; }
             }
     }
     const float inv = L == 0.f ? 0.f : 1.f / L;
@@ -681,13 +685,22 @@ __device__ __forceinline__ void kv8_sum(const float *p0, int NS, int tt, int hh,
     for (int e = 0; e < 8; ++e) o[e] *= inv;
 }
 
-// Smallest and largest over the 32 rows of a tile of what they see; rows that see nothing count as none.
+// The number of a sequence's page u; -1 for one that is no page's.  It is asked for before the loads of an earlier page and made
+// uniform (waited for) behind them: a wait where it is asked for is one for every load of the wave that is on its way.
+__device__ __forceinline__ int kv8_ask(const Kv8State &s, const int *table, int u) { return table[min(u, s.max_blocks - 1)]; }
+__device__ __forceinline__ int kv8_page(const Kv8State &s, int asked) {
+    const int id = __builtin_amdgcn_readfirstlane(asked);
+    return (unsigned)id < (unsigned)s.n_pages ? id : -1;
+}
+
+// Smallest and largest over the rows of a tile (the lanes of a group of ROWS) of what they see; rows that see nothing count as none.
 struct Kv8Span { int min8, max8, hmin, hmax; };     // 8-bit keys all rows see / some row sees; hot pages [hmin, hmax]
+template <int ROWS>
 __device__ __forceinline__ Kv8Span kv8_span(const Kv8Row &r) {
     const bool sees = r.lim > 0, warm = sees && r.h0 < r.lim;
     Kv8Span s{sees ? r.lim8 : 0x7fffffff, r.lim8, warm ? r.h0 / KV8_PAGE : 0x7fffffff, warm ? r.h0 / KV8_PAGE : -1};
 #pragma unroll
-    for (int off = 1; off < 32; off <<= 1) {
+    for (int off = 1; off < ROWS; off <<= 1) {
         s.min8 = min(s.min8, shx(s.min8, off)); s.max8 = max(s.max8, shx(s.max8, off));
         s.hmin = min(s.hmin, shx(s.hmin, off)); s.hmax = max(s.hmax, shx(s.hmax, off));
     }
@@ -696,169 +709,280 @@ __device__ __forceinline__ Kv8Span kv8_span(const Kv8Row &r) {
     return s;
 }
 
-// Few packed rows (decoding): one tile of 32 per workgroup, whose eight waves share the pages of a key range; a wave streams its pages
-// straight to registers.  The launch is a chain of latencies where contexts are short, so a wave asks for its first page's number
-// before it knows what its rows see, and for the page before it has asked for Q; and a stream of memory where they are long: each
-// wave has half a page or more (8 KB with head_dim 128) on its way, K of the next page during the softmax, V during the next products.
+// Few packed rows (decoding): a tile of 16 per workgroup, whose four waves share the pages of a key range; a wave streams its pages
+// straight to registers.  The products are 16 x 16 x 32: one token of a group of four fills a quarter of the operand's rows, of
+// 32 x 32 x 16 an eighth, and O, Q and the scores take half the registers, so that no wave keeps any in memory, where each
+// reload would wait for all pages that are on their way.  The launch is a chain of latencies where contexts are short: a wave
+// asks for its first page before it knows what its rows see.  Where they are long it is a stream of memory: each wave has half a page or
+// more (8 KB with head_dim 128) on its way, K of the next page during the softmax, V during the next scores.
 // The waves' results meet in LDS and, with several key ranges, in memory, where the last workgroup to arrive adds them up.
-// grid: x = kv head + Hkv * key range, y tile, z sequence; 512 threads
-template <int HD, int SRC>
-__global__ __launch_bounds__(512, 1) void k_kv8_attn_few(const Kv8Attn a) {
-    constexpr int KSQ = HD / 16, HT = HD / 32, N = Kv8Planes<HD, SRC>::N, KC = HD / 32, W = 8;   // KC chunks per 32 keys of K, and of V
-    __shared__ float s_o[4][HT * 16][64];
-    __shared__ float s_ml[W][2][32];
+// Operands (lane: n = lane % 16, g = lane / 16): a K operand's row 4 a + i is key 8 a + 4 kb + i of 32, so that a lane of S^T holds
+// keys 8 g .. + 7 of each tile of 32, which is the P operand's order; a lane's eight bytes are half of a chunk's sixteen.
+// STREAM: the sequence has no other tile (launches of several tiles read a page once per tile, from L2).
+// grid: x = kv head + Hkv * key range, y tile, z sequence; 256 threads
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+__device__ __forceinline__ f32x4 mfma16(uint4 a, uint4 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+// eight bytes that nobody else of this launch reads: not to be kept in L2
+__device__ __forceinline__ uint2 load8_stream(const uint8_t *p) {
+    typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
+    const u32x2 x = __builtin_nontemporal_load((const u32x2 *)p);
+    return make_uint2(x.x, x.y);
+}
+template <int HD>
+struct Kv8Part16 { static constexpr int FLOATS = 16 * HD + 32; };   // per (tile of 16, kv head, range): O [HD/16][64 lanes][4], (M, L)[16]
+
+template <int HD, int SRC, bool STREAM>
+__global__ __launch_bounds__(256, HD == 128 && SRC != KV8_BF16 ? 2 : 3) void k_kv8_attn_few(const Kv8Attn a) {
+    constexpr int T = HD / 32, CB = HD / 16, N = Kv8Planes<HD, SRC>::N, PF = Kv8Part16<HD>::FLOATS;   // T: k-steps of 32, and chunks per 32 keys
+    constexpr int W = 4, NB = (CB + W - 1) / W;        // waves; channel blocks that a wave adds up
+    __shared__ float4 s_o[4][CB][64];
+    __shared__ float s_ml[W][2][16];
     __shared__ int s_flag;
     const int tidx = opaque_tid();
-    const int w = __builtin_amdgcn_readfirstlane(tidx >> 6), lane = tidx & 63, half = lane >> 5;
+    const int w = __builtin_amdgcn_readfirstlane(tidx >> 6), lane = tidx & 63, n = lane & 15, g = lane >> 4;
     const int b = blockIdx.z, rt = blockIdx.y, kvh = blockIdx.x % opaque_s(a.Hkv), split = blockIdx.x / opaque_s(a.Hkv);
-    const int stride = W * a.NS, *table = a.s.table + (size_t)b * a.s.max_blocks;
+    const int stride = W * a.NS;
+    const int *table = a.s.table + (size_t)b * a.s.max_blocks;
     int u = split * W + w;
-    auto page_of = [&](int i) { return __builtin_amdgcn_readfirstlane(table[min(i, a.s.max_blocks - 1)]); };
-    auto valid = [&](int id) { return (unsigned)id < (unsigned)a.s.n_pages; };
-    auto base_of = [&](int i) { return (size_t)(valid(i) ? i : 0) * a.Hkv + kvh; };   // (a page that does not exist is read as page 0 and masked)
-    uint4 kc[2 * KC], vc[2 * KC];
+    const int ask0 = kv8_ask(a.s, table, u);
+    int ask = kv8_ask(a.s, table, u + stride);
+    // a lane's place in a chunk: storage row of its key (kb = 0; kb = 1: 8 rows on), half and octet of the elements
+    const int krow = (n & 3) + 4 * (n >> 3) + 8 * ((n >> 1) & 2);
+    const int k_off = ((g & 1) * 32 + krow) * 16 + 8 * (g >> 1), v_off = ((g >> 1) * 32 + n) * 16 + 8 * (g & 1);
+    uint2 kc[2][2][T], vc[2][CB];
     float ks1, vs1;
-    auto load_k = [&](int i) {
-        const uint4 *p = (const uint4 *)(a.pages + base_of(i) * (2 * KV8_PAGE * HD)) + lane;
-#pragma unroll
-        for (int c = 0; c < 2 * KC; ++c) kc[c] = p[c * 64];
-        ks1 = a.scales[base_of(i) * 2];
-    };
-    auto load_v = [&](int i) {
-        const uint4 *p = (const uint4 *)(a.pages + base_of(i) * (2 * KV8_PAGE * HD) + KV8_PAGE * HD) + lane;
-#pragma unroll
-        for (int c = 0; c < 2 * KC; ++c) vc[c] = p[c * 64];
-        vs1 = a.scales[base_of(i) * 2 + 1];
-    };
-    int id = page_of(u), id1 = page_of(u + stride);
-    if (rt * 32 >= (a.s.cu[b + 1] - a.s.cu[b]) * a.G) return;
-    load_k(id);
-    const Kv8Row r = kv8_row(a, b, kvh, rt * 32 + (lane & 31));
-    uint4 q[N][KSQ];
-    kv8_load_q<HD, SRC>(a, r, b, half, q);
-    load_v(id);
-    const Kv8Span sp = kv8_span(r);
-    f32x16 oacc[HT];
-#pragma unroll
-    for (int tt = 0; tt < HT; ++tt)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) oacc[tt][e] = 0.f;
-    float m_run = a.m_init, l_run = 0.f;
-    auto scores = [&](f32x16 (&sacc)[2], auto frag) {     // frag(tile, k-step): a K fragment in bf16
+    auto get = [](const uint8_t *p) { return STREAM ? load8_stream(p) : *(const uint2 *)p; };
+    auto load_k = [&](int id) {
+        const size_t at = (size_t)max(id, 0) * a.Hkv + kvh;      // (a page that does not exist is read as page 0 and masked)
+        const uint8_t *p = a.pages + at * (2 * KV8_PAGE * HD) + k_off;
 #pragma unroll
         for (int j = 0; j < 2; ++j)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) sacc[j][e] = 0.f;
+            for (int t = 0; t < T; ++t)
 #pragma unroll
-        for (int s = 0; s < KSQ; ++s) {
-            const uint4 k0 = frag(0, s), k1 = frag(1, s);
-#pragma unroll
-            for (int p = 0; p < N; ++p) { sacc[0] = mfma32(k0, q[p][s], sacc[0]); sacc[1] = mfma32(k1, q[p][s], sacc[1]); }
-        }
+                for (int kb = 0; kb < 2; ++kb) kc[j][kb][t] = get(p + (j * T + t) * 1024 + kb * 128);
+        ks1 = a.scales[at * 2];
     };
-    auto values = [&](const f32x16 (&sacc)[2], auto frag) {   // frag(tile, channel tile, step): a V^T fragment
+    auto load_v = [&](int id) {
+        const size_t at = (size_t)max(id, 0) * a.Hkv + kvh;
+        const uint8_t *p = a.pages + at * (2 * KV8_PAGE * HD) + KV8_PAGE * HD + v_off;
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int c = 0; c < CB; ++c) vc[j][c] = get(p + (j * T + (c >> 1)) * 1024 + (c & 1) * 256);
+        vs1 = a.scales[at * 2 + 1];
+    };
+    int id = kv8_page(a.s, ask0);
+    if (rt * 16 >= (a.s.cu[b + 1] - a.s.cu[b]) * a.G) return;
+    load_k(id);
+    const Kv8Row r = kv8_row(a, b, kvh, rt * 16 + n);
+    uint4 q[N][T];
+#pragma unroll
+    for (int t = 0; t < T; ++t) {
+        uint4 o[N];
+        kv8_q8<HD, SRC>(a, r, b, 32 * t + 16 * (g >> 1) + 8 * (g & 1), o);
+#pragma unroll
+        for (int p = 0; p < N; ++p) q[p][t] = o[p];
+    }
+    load_v(id);
+    const Kv8Span sp = kv8_span<16>(r);
+    const f32x4 zero4 = {0.f, 0.f, 0.f, 0.f};
+    f32x4 oacc[CB];
+#pragma unroll
+    for (int c = 0; c < CB; ++c) oacc[c] = zero4;
+    float m_run = a.m_init, l_run = 0.f;
+    // scores of 64 keys to weights and result: kf(tile, kb, step), vf(tile, channel block): fragments in bf16
+    auto scores = [&](f32x4 (&s)[2][2], auto kf) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb) {
+                s[j][kb] = zero4;
+#pragma unroll
+                for (int t = 0; t < T; ++t) {
+                    const uint4 k = kf(j, kb, t);
+#pragma unroll
+                    for (int p = 0; p < N; ++p) s[j][kb] = mfma16(k, q[p][t], s[j][kb]);
+                }
+            }
+    };
+    auto softmax = [&](f32x4 (&s)[2][2], bool mask, int page, int hi) {
+        if (mask) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (page * KV8_PAGE + 32 * j + 8 * g + 4 * kb + i >= hi) s[j][kb][i] = -INFINITY;
+        }
+        float mx = s[0][0][0];
+#pragma unroll
+        for (int e = 1; e < 16; ++e) mx = fmaxf(mx, s[e >> 3][(e >> 2) & 1][e & 3]);
+        if (__builtin_amdgcn_ballot_w64((mx - m_run) * a.scale_log2e > KV8_SLACK)) {     // (see kv8_rescale)
+            mx = fmaxf(mx, shx(mx, 16));
+            const float m_new = fmaxf(m_run, fmaxf(mx, shx(mx, 32)));
+            const float alpha = __builtin_amdgcn_exp2f((m_run - m_new) * a.scale_log2e);
+            m_run = m_new;
+            l_run *= alpha;
+#pragma unroll
+            for (int c = 0; c < CB; ++c) oacc[c] *= alpha;
+        }
+        const float mb = m_run * a.scale_log2e;
+        float ls = 0.f;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const float x = __builtin_amdgcn_exp2f(fmaf(s[e >> 3][(e >> 2) & 1][e & 3], a.scale_log2e, -mb));
+            s[e >> 3][(e >> 2) & 1][e & 3] = x;
+            ls += x;
+        }
+        l_run += ls;
+    };
+    auto values = [&](const f32x4 (&s)[2][2], auto vf) {
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            float pr[16];
+            const float pr[8] = {s[j][0][0], s[j][0][1], s[j][0][2], s[j][0][3], s[j][1][0], s[j][1][1], s[j][1][2], s[j][1][3]};
+            uint4 ph[N];
+            split_planes<N>(pr, ph);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) pr[e] = sacc[j][e];
-            uint4 ph[2][N];
-            split_planes<N>(pr, ph[0]);
-            split_planes<N>(pr + 8, ph[1]);
+            for (int c = 0; c < CB; ++c) {
+                const uint4 v = vf(j, c);
 #pragma unroll
-            for (int s2 = 0; s2 < 2; ++s2)
-#pragma unroll
-                for (int tt = 0; tt < HT; ++tt) {
-                    const uint4 v = frag(j, tt, s2);
-#pragma unroll
-                    for (int p = 0; p < N; ++p) oacc[tt] = mfma32(v, ph[s2][p], oacc[tt]);
-                }
+                for (int p = 0; p < N; ++p) oacc[c] = mfma16(v, ph[p], oacc[c]);
+            }
         }
     };
     const int n8 = (sp.max8 + KV8_PAGE - 1) / KV8_PAGE, nh = max(0, sp.hmax - sp.hmin + 1);
+    f32x4 s[2][2];
     for (; u < n8; u += stride) {
-        const int id2 = page_of(u + 2 * stride);
-        const bool live = valid(id);
+        const bool live = id >= 0;
+        const int ask2 = kv8_ask(a.s, table, u + 2 * stride);
         const float ks = ks1, vs = vs1;
-        f32x16 sacc[2];
-        scores(sacc, [&](int j, int s) {
-            const uint4 c = kc[j * KC + (s >> 1)];
-            return s & 1 ? dequant8(c.z, c.w, ks) : dequant8(c.x, c.y, ks);
-        });
+        scores(s, [&](int j, int kb, int t) { return dequant8(kc[j][kb][t].x, kc[j][kb][t].y, ks); });
+        const int id1 = kv8_page(a.s, ask);
         if (u + stride < n8) load_k(id1);
-        const int key0 = u * KV8_PAGE + 16 * half;
-        kv8_softmax<HT>(sacc, (u + 1) * KV8_PAGE > sp.min8 || !live, key0, 0, live ? r.lim8 : 0, a.scale_log2e, m_run, l_run, oacc);
-        values(sacc, [&](int j, int tt, int s2) {
-            const uint4 c = vc[j * KC + tt];
-            return s2 ? dequant8(c.z, c.w, vs) : dequant8(c.x, c.y, vs);
-        });
+        softmax(s, (u + 1) * KV8_PAGE > sp.min8 || !live, u, live ? r.lim8 : 0);
+        values(s, [&](int j, int c) { return dequant8(vc[j][c].x, vc[j][c].y, vs); });
         if (u + stride < n8) load_v(id1);
-        id = id1; id1 = id2;
+        id = id1; ask = ask2;
     }
     for (; u < n8 + nh; u += stride) {       // hot pages
         const int page = sp.hmin + u - n8;
         const size_t off = (size_t)b * a.hot.seq_stride + (size_t)kvh * a.hot.head_stride + (size_t)((page * KV8_PAGE + a.s.hotbase[b]) & a.hot.mask) * HD;
-        const uint4 *kp = (const uint4 *)(a.hot.k + off) + lane, *vp = (const uint4 *)(a.hot.v + off) + lane;
-        f32x16 sacc[2];
-        scores(sacc, [&](int j, int s) { return kp[(j * KSQ + s) * 64]; });
-        const int own = r.h0 < r.lim && r.h0 / KV8_PAGE == page;
-        kv8_softmax<HT>(sacc, true, page * KV8_PAGE + 16 * half, 0, own ? r.lim : 0, a.scale_log2e, m_run, l_run, oacc);
-        values(sacc, [&](int j, int tt, int s2) { return vp[(j * KSQ + tt * 2 + s2) * 64]; });
+        const uint4 *kp = (const uint4 *)(a.hot.k + off) + (g & 1) * 32 + krow, *vp = (const uint4 *)(a.hot.v + off) + (g >> 1) * 32 + n;
+        scores(s, [&](int j, int kb, int t) { return kp[(j * CB + 2 * t + (g >> 1)) * 64 + 8 * kb]; });
+        softmax(s, true, page, r.h0 < r.lim && r.h0 / KV8_PAGE == page ? r.lim : 0);
+        values(s, [&](int j, int c) { return vp[(j * CB + (c >> 1) * 2 + (g & 1)) * 64 + (c & 1) * 16]; });
     }
-    // the waves' shares: waves 4 .. 7 hand theirs to waves 0 .. 3, then every wave adds up eight registers of a tile
-    const float l_tot = l_run + shx(l_run, 32);
-    if (lane < 32) { s_ml[w][0][lane] = m_run; s_ml[w][1][lane] = l_tot; }
+    // the waves' shares meet: every wave adds up a part of the channels
+    l_run += shx(l_run, 16);
+    l_run += shx(l_run, 32);
+    if (lane < 16) { s_ml[w][0][lane] = m_run; s_ml[w][1][lane] = l_run; }
     __syncthreads();
     float M = a.m_init, L = 0.f;
 #pragma unroll
-    for (int i = 0; i < W; ++i) M = fmaxf(M, s_ml[i][0][lane & 31]);
+    for (int i = 0; i < W; ++i) M = fmaxf(M, s_ml[i][0][n]);
 #pragma unroll
-    for (int i = 0; i < W; ++i) L += s_ml[i][1][lane & 31] * __builtin_amdgcn_exp2f((s_ml[i][0][lane & 31] - M) * a.scale_log2e);
+    for (int i = 0; i < W; ++i) L += s_ml[i][1][n] * __builtin_amdgcn_exp2f((s_ml[i][0][n] - M) * a.scale_log2e);
     const float f = __builtin_amdgcn_exp2f((m_run - M) * a.scale_log2e);
-    if (w >= 4)
+    auto scaled = [&](int c) { return make_float4(oacc[c][0] * f, oacc[c][1] * f, oacc[c][2] * f, oacc[c][3] * f); };
 #pragma unroll
-        for (int tt = 0; tt < HT; ++tt)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) s_o[w - 4][tt * 16 + e][lane] = oacc[tt][e] * f;
+    for (int c = 0; c < CB; ++c) s_o[w][c][lane] = scaled(c);
     __syncthreads();
-    if (w < 4)
+    float o[NB][4];
 #pragma unroll
-        for (int tt = 0; tt < HT; ++tt)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) s_o[w][tt * 16 + e][lane] += oacc[tt][e] * f;
-    __syncthreads();
-    const int tt = w >> 1, hh = w & 1;
-    const bool on = tt < HT;
-    float o[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const int i = min(tt, HT - 1) * 16 + 8 * hh + e;
-        o[e] = (s_o[0][i][lane] + s_o[1][i][lane]) + (s_o[2][i][lane] + s_o[3][i][lane]);
+    for (int k = 0; k < NB; ++k) {
+        const int cb = min(w + k * W, CB - 1);
+        const float4 x0 = s_o[0][cb][lane], x1 = s_o[1][cb][lane], x2 = s_o[2][cb][lane], x3 = s_o[3][cb][lane];
+        o[k][0] = (x0.x + x1.x) + (x2.x + x3.x); o[k][1] = (x0.y + x1.y) + (x2.y + x3.y);
+        o[k][2] = (x0.z + x1.z) + (x2.z + x3.z); o[k][3] = (x0.w + x1.w) + (x2.w + x3.w);
     }
     if (a.NS > 1) {
         const size_t item = (size_t)(b * a.rts + rt) * a.Hkv + kvh;
-        float *p0 = a.part + item * a.NS * AttnPartial<HD>::FLOATS, *pp = p0 + (size_t)split * AttnPartial<HD>::FLOATS;
-        if (on && r.row >= 0) kv8_put<HD>(pp, tt, hh, o, lane);
-        if (w == 0 && lane < 32 && r.row >= 0) st_agent2(pp + 32 * HD + 2 * lane, M, L);
-        if (!arrive_last(a.counters + item, a.NS, &s_flag) || !on) return;
-        if (r.row >= 0) kv8_sum<HD, true>(p0, a.NS, tt, hh, lane, a.m_init, a.scale_log2e, o);
-    } else {
-        const float inv = L == 0.f ? 0.f : 1.f / L;
+        float *p0 = a.part + item * a.NS * PF, *pp = p0 + (size_t)split * PF;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) o[e] *= inv;
+        for (int k = 0; k < NB; ++k)
+            if (w + k * W < CB && r.row >= 0) store16_agent(pp + ((w + k * W) * 64 + lane) * 4, o[k][0], o[k][1], o[k][2], o[k][3]);
+        if (w == 0 && lane < 16 && r.row >= 0) st_agent2(pp + 16 * HD + 2 * lane, M, L);
+        if (!arrive_last(a.counters + item, a.NS, &s_flag)) return;
+        constexpr int CH = 8 / NB;       // ranges requested together
+        M = a.m_init; L = 0.f;
+#pragma unroll
+        for (int k = 0; k < NB; ++k)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[k][e] = 0.f;
+        if (r.row >= 0)
+            for (int s0 = 0; s0 < a.NS; s0 += CH) {
+                float2 x[CH], v[CH][NB][2];
+#pragma unroll
+                for (int i = 0; i < CH; ++i) {
+                    const float *ps = p0 + (size_t)min(s0 + i, a.NS - 1) * PF;
+                    x[i] = ld_agent2(ps + 16 * HD + 2 * n);
+#pragma unroll
+                    for (int k = 0; k < NB; ++k) {
+                        const float *po = ps + (min(w + k * W, CB - 1) * 64 + lane) * 4;
+                        v[i][k][0] = ld_agent2(po);
+                        v[i][k][1] = ld_agent2(po + 2);
+                    }
+                }
+                float mn = M;
+#pragma unroll
+                for (int i = 0; i < CH; ++i) mn = fmaxf(mn, x[i].x);
+                const float f0 = __builtin_amdgcn_exp2f((M - mn) * a.scale_log2e);
+                M = mn;
+                L *= f0;
+#pragma unroll
+                for (int k = 0; k < NB; ++k)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[k][e] *= f0;
+#pragma unroll
+                for (int i = 0; i < CH; ++i)
+                    if (s0 + i < a.NS) {
+                        const float fi = __builtin_amdgcn_exp2f((x[i].x - M) * a.scale_log2e);
+                        L += fi * x[i].y;
+#pragma unroll
+                        for (int k = 0; k < NB; ++k) { o[k][0] += fi * v[i][k][0].x; o[k][1] += fi * v[i][k][0].y; o[k][2] += fi * v[i][k][1].x; o[k][3] += fi * v[i][k][1].y; }
+                    }
+            }
     }
-    if (on) kv8_store<HD, SRC>(a, r, tt, hh, o, lane);
+    const float inv = L == 0.f ? 0.f : 1.f / L;
+#pragma unroll
+    for (int k = 0; k < NB; ++k) {
+        if (w + k * W >= CB) break;
+        // (a row that sees nothing is not masked where the others of its tile need no mask)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[k][e] = r.lim > 0 ? o[k][e] * inv : 0.f;
+        const int ch = (w + k * W) * 16 + 4 * g;
+        if constexpr (SRC == KV8_FRAG) {     // lanes 16 apart hold the two halves of an octet: one writes its high plane, one its low
+            const float x0 = shx(o[k][0], 16), x1 = shx(o[k][1], 16), x2 = shx(o[k][2], 16), x3 = shx(o[k][3], 16);
+            const bool odd = g & 1;
+            const float v8[8] = {odd ? x0 : o[k][0], odd ? x1 : o[k][1], odd ? x2 : o[k][2], odd ? x3 : o[k][3], odd ? o[k][0] : x0, odd ? o[k][1] : x1, odd ? o[k][2] : x2, odd ? o[k][3] : x3};
+            uint4 hi, lo;
+            pack8_split(v8, hi, lo);
+            if (r.row >= 0) {
+                const size_t vec = (size_t)(r.row >> 5) * (a.Hq * HD / 16) * 64 + frag_vec(r.row & 31, r.head * (HD / 8) + (ch >> 3));
+                if (odd) a.xlo[vec] = lo; else a.xhi[vec] = hi;
+            }
+        } else if (r.row >= 0) {
+            const size_t at = (size_t)r.row * a.out_stride + r.head * HD + ch;
+            if constexpr (SRC == KV8_BF16) *(uint2 *)((uint16_t *)a.out + at) = make_uint2(f2bf2(o[k][0], o[k][1]), f2bf2(o[k][2], o[k][3]));
+            else *(float4 *)((float *)a.out + at) = make_float4(o[k][0], o[k][1], o[k][2], o[k][3]);
+        }
+    }
 }
 
 // Many packed rows (blocks of a group, prompts): four tiles of 32 per workgroup, one per wave; a page is made bf16 once by all four, in
-// LDS, double-buffered with one barrier per page: page i + 1 goes from registers to LDS and page i + 2 from memory to registers
-// under the products of page i.  grid: x = kv head + Hkv * key range, y group of four tiles counted from the last (prompts: the
-// longest start first), z sequence; 256 threads
+// LDS.  A step multiplies Q with the keys of page u + 1 under the softmax of page u, whose matrix and vector work do not wait for each
+// other, then adds page u's values: K is staged two pages ahead and V one (two waves stage K, two V; from memory to registers one
+// more page ahead), with one barrier per page.  grid: x = kv head + Hkv * key range, y group of four tiles counted from the last
+// (prompts: the longest start first), z sequence; 256 threads
 template <int HD, int SRC>
 __global__ __launch_bounds__(256, HD == 128 && SRC == KV8_F32 ? 1 : 2) void k_kv8_attn_many(const Kv8Attn a) {
     constexpr int KSQ = HD / 16, HT = HD / 32, N = Kv8Planes<HD, SRC>::N, FR = HD / 8;    // FR fragments of 1 KB of K, and of V, per page
     constexpr int LPW = HD / 32;           // chunks per wave and page; of the HD / 8 chunks the first half is K
-    __shared__ __attribute__((aligned(16))) uint4 buf[2][2 * FR * 64];
+    __shared__ __attribute__((aligned(16))) uint4 buf[2][2][FR * 64];      // [K, V][page mod 2]
     __shared__ int s_span[4][4];
     const int tidx = opaque_tid();
     const int w = __builtin_amdgcn_readfirstlane(tidx >> 6), lane = tidx & 63, half = lane >> 5;
@@ -868,7 +992,7 @@ __global__ __launch_bounds__(256, HD == 128 && SRC == KV8_F32 ? 1 : 2) void k_kv
     const int rt = rt0 + w;
     const bool active = rt * 32 < packed;
     const Kv8Row r = kv8_row(a, b, kvh, rt * 32 + (lane & 31));
-    const Kv8Span sp = kv8_span(r);
+    const Kv8Span sp = kv8_span<32>(r);
     if (lane == 0) { s_span[w][0] = sp.max8; s_span[w][1] = sp.hmin; s_span[w][2] = sp.hmax; }
     __syncthreads();
     int max8 = 0, hmin = 0x7fffffff, hmax = -1;
@@ -886,28 +1010,26 @@ __global__ __launch_bounds__(256, HD == 128 && SRC == KV8_F32 ? 1 : 2) void k_kv
     const int n8 = (max8 + KV8_PAGE - 1) / KV8_PAGE, nh = max(0, hmax - hmin + 1), n = n8 + nh;
     const int per = (n + a.NS - 1) / opaque_s(a.NS), u0 = split * per, u1 = min(n, u0 + per);
     const int *table = a.s.table + (size_t)b * a.s.max_blocks;
-    auto valid = [&](int id) { return (unsigned)id < (unsigned)a.s.n_pages; };
-    // what a wave holds of the page on its way: 8-bit chunks with their scale, or bf16 fragments
-    uint4 raw[2 * LPW];
+    int ask = kv8_ask(a.s, table, u0);
+    uint32_t live = 0;       // bit u % 32: page u exists
+    // what a wave holds of the page on its way: 8-bit chunks with their scale.  (A hot page, of which a workgroup has one or two, is
+    // read when it is placed: registers for its fragments on their way would be missing in the products.)
+    uint4 raw[LPW];
     float raw_scale = 1.f;
     const bool is_v = w >= 2;
     auto fetch = [&](int u) {
-        if (u < n8) {
-            const int t = __builtin_amdgcn_readfirstlane(table[u]);
-            const size_t at = (size_t)(valid(t) ? t : 0) * a.Hkv + kvh;
-            const uint4 *p = (const uint4 *)(a.pages + at * (2 * KV8_PAGE * HD)) + w * LPW * 64 + lane;
+        if (u >= n8) return;
+        const int id = kv8_page(a.s, ask);
+        ask = kv8_ask(a.s, table, u + 1);
+        live = id >= 0 ? live | 1u << (u & 31) : live & ~(1u << (u & 31));
+        const size_t at = (size_t)max(id, 0) * a.Hkv + kvh;      // (a page that does not exist is read as page 0 and masked)
+        const uint4 *p = (const uint4 *)(a.pages + at * (2 * KV8_PAGE * HD)) + w * LPW * 64 + lane;
 #pragma unroll
-            for (int c = 0; c < LPW; ++c) raw[c] = p[c * 64];
-            raw_scale = a.scales[at * 2 + is_v];
-        } else {
-            const size_t off = (size_t)b * a.hot.seq_stride + (size_t)kvh * a.hot.head_stride + (size_t)(((hmin + u - n8) * KV8_PAGE + a.s.hotbase[b]) & a.hot.mask) * HD;
-            const uint4 *p = (const uint4 *)((is_v ? a.hot.v : a.hot.k) + off) + (w & 1) * 2 * LPW * 64 + lane;
-#pragma unroll
-            for (int c = 0; c < 2 * LPW; ++c) raw[c] = p[c * 64];
-        }
+        for (int c = 0; c < LPW; ++c) raw[c] = p[c * 64];
+        raw_scale = a.scales[at * 2 + is_v];
     };
     auto place = [&](int u) {
-        uint4 *d = buf[u & 1] + w * 2 * LPW * 64 + lane;
+        uint4 *d = buf[is_v][u & 1] + (w & 1) * 2 * LPW * 64 + lane;
         if (u < n8) {
 #pragma unroll
             for (int c = 0; c < LPW; ++c) {
@@ -915,54 +1037,100 @@ __global__ __launch_bounds__(256, HD == 128 && SRC == KV8_F32 ? 1 : 2) void k_kv
                 d[(2 * c + 1) * 64] = dequant8(raw[c].z, raw[c].w, raw_scale);
             }
         } else {
+            const size_t off = (size_t)b * a.hot.seq_stride + (size_t)kvh * a.hot.head_stride + (size_t)(((hmin + u - n8) * KV8_PAGE + a.s.hotbase[b]) & a.hot.mask) * HD;
+            const uint4 *p = (const uint4 *)((is_v ? a.hot.v : a.hot.k) + off) + (w & 1) * 2 * LPW * 64 + lane;
 #pragma unroll
-            for (int c = 0; c < 2 * LPW; ++c) d[c * 64] = raw[c];
+            for (int h = 0; h < 2; ++h) {
+                uint4 x[LPW];
+#pragma unroll
+                for (int c = 0; c < LPW; ++c) x[c] = p[(h * LPW + c) * 64];
+#pragma unroll
+                for (int c = 0; c < LPW; ++c) d[(h * LPW + c) * 64] = x[c];
+            }
         }
     };
-    if (u0 < u1) {
-        fetch(u0);
-        place(u0);
-        if (u0 + 1 < u1) fetch(u0 + 1);
-    }
-    for (int u = u0; u < u1; ++u) {
-        __syncthreads();      // page u is in LDS, and page u - 1 has been read by all
-        if (u + 1 < u1) { place(u + 1); if (u + 2 < u1) fetch(u + 2); }
-        const bool cold = u < n8;
-        const int page = cold ? u : hmin + u - n8;
-        int lo = 0, hi = cold ? r.lim8 : (r.h0 < r.lim && r.h0 / KV8_PAGE == page ? r.lim : 0);
-        if (cold && !valid(__builtin_amdgcn_readfirstlane(table[u]))) hi = 0;
-        const bool mask = !cold || (u + 1) * KV8_PAGE > sp.min8 || hi == 0;
-        if (!active || (cold && u * KV8_PAGE >= sp.max8) || (!cold && (page < sp.hmin || page > sp.hmax))) continue;
-        const uint4 *fr = buf[u & 1] + lane;
-        f32x16 sacc[2];
+    // Products in groups of two k-steps (four fragments); the next group's fragments are read first and the caller's vector work fills
+    // the matrix instructions' time.
+    constexpr int GK = KSQ / 2;
+    auto scores = [&](f32x16 (&sacc)[2], int u, auto beside) {
+        const uint4 *fr = buf[0][u & 1] + lane;
+        uint4 k[2][4];
+        auto read = [&](int g, uint4 (&d)[4]) { d[0] = fr[2 * g * 64]; d[1] = fr[(KSQ + 2 * g) * 64]; d[2] = fr[(2 * g + 1) * 64]; d[3] = fr[(KSQ + 2 * g + 1) * 64]; };
+        read(0, k[0]);
 #pragma unroll
         for (int j = 0; j < 2; ++j)
 #pragma unroll
             for (int e = 0; e < 16; ++e) sacc[j][e] = 0.f;
 #pragma unroll
-        for (int s = 0; s < KSQ; ++s) {
-            const uint4 k0 = fr[s * 64], k1 = fr[(KSQ + s) * 64];
+        for (int g = 0; g < GK; ++g) {
+            __builtin_amdgcn_sched_barrier(0);
+            if (g + 1 < GK) read(g + 1, k[(g + 1) & 1]);
 #pragma unroll
-            for (int p = 0; p < N; ++p) { sacc[0] = mfma32(k0, q[p][s], sacc[0]); sacc[1] = mfma32(k1, q[p][s], sacc[1]); }
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int p = 0; p < N; ++p) { sacc[0] = mfma32(k[g & 1][2 * s], q[p][2 * g + s], sacc[0]); sacc[1] = mfma32(k[g & 1][2 * s + 1], q[p][2 * g + s], sacc[1]); }
+            beside(g);
+            __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+            for (int i = 0; i < 4 * N; ++i) { __builtin_amdgcn_sched_group_barrier(0x8, 1, 0); __builtin_amdgcn_sched_group_barrier(0x2, 24 / GK / N, 0); }
         }
-        kv8_softmax<HT>(sacc, __builtin_amdgcn_ballot_w64(mask) != 0, page * KV8_PAGE + 16 * half, lo, hi, a.scale_log2e, m_run, l_run, oacc);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    const int ahead = is_v ? 1 : 2;      // pages that this wave stages ahead of the one whose values are added
+    f32x16 sacc[2];
+    if (u0 < u1) {
+        fetch(u0);
+        place(u0);
+        if (u0 + 1 < u1) fetch(u0 + 1);
+        if (!is_v && u0 + 1 < u1) { place(u0 + 1); if (u0 + 2 < u1) fetch(u0 + 2); }
+        __syncthreads();
+        if (active) scores(sacc, u0, [](int) {});
+    }
+    auto step = [&](int u, f32x16 (&sacc)[2], f32x16 (&nacc)[2]) {     // sacc: page u's scores; nacc: the next page's
+        __syncthreads();      // page u + 1's keys and page u's values are in LDS; page u's keys and u - 1's values have been read
+        if (u + ahead < u1) { place(u + ahead); if (u + ahead + 1 < u1) fetch(u + ahead + 1); }
+        if (!active) return;
+        const bool cold = u < n8;
+        const int page = cold ? u : hmin + u - n8;
+        int hi = cold ? r.lim8 : (r.h0 < r.lim && r.h0 / KV8_PAGE == page ? r.lim : 0);
+        if (cold && !(live >> (u & 31) & 1)) hi = 0;
+        kv8_rescale<HT>(sacc, __builtin_amdgcn_ballot_w64(r.lim > 0 && (page + 1) * KV8_PAGE > hi) != 0, page * KV8_PAGE + 16 * half, hi, a.scale_log2e, m_run, l_run, oacc);
+        const float mb = m_run * a.scale_log2e;
+        float ls[2] = {0.f, 0.f};
+        scores(nacc, min(u + 1, u1 - 1), [&](int g) {       // the weights of page u, a share beside every group
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            float pr[16];
+            for (int e = 16 / GK * g; e < 16 / GK * (g + 1); ++e)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) pr[e] = sacc[j][e];
-            uint4 ph[2][N];
-            split_planes<N>(pr, ph[0]);
-            split_planes<N>(pr + 8, ph[1]);
+                for (int j = 0; j < 2; ++j) { sacc[j][e] = __builtin_amdgcn_exp2f(fmaf(sacc[j][e], a.scale_log2e, -mb)); ls[j] += sacc[j][e]; }
+        });
+        l_run += ls[0] + ls[1];
+        const uint4 *fr = buf[1][u & 1] + lane;
+        uint4 v[2][HT];
+        auto read = [&](int g, uint4 (&d)[HT]) {       // g = 2 * tile + step
 #pragma unroll
-            for (int s2 = 0; s2 < 2; ++s2)
+            for (int tt = 0; tt < HT; ++tt) d[tt] = fr[((g >> 1) * KSQ + tt * 2 + (g & 1)) * 64];
+        };
+        read(0, v[0]);
 #pragma unroll
-                for (int tt = 0; tt < HT; ++tt) {
-                    const uint4 v = fr[(FR + j * KSQ + tt * 2 + s2) * 64];
+        for (int g = 0; g < 4; ++g) {
+            __builtin_amdgcn_sched_barrier(0);
+            if (g < 3) read(g + 1, v[(g + 1) & 1]);
+            float pr[8];
 #pragma unroll
-                    for (int p = 0; p < N; ++p) oacc[tt] = mfma32(v, ph[s2][p], oacc[tt]);
-                }
+            for (int e = 0; e < 8; ++e) pr[e] = sacc[g >> 1][8 * (g & 1) + e];
+            uint4 ph[N];
+            split_planes<N>(pr, ph);
+#pragma unroll
+            for (int p = 0; p < N; ++p)
+#pragma unroll
+                for (int tt = 0; tt < HT; ++tt) oacc[tt] = mfma32(v[g & 1][tt], ph[p], oacc[tt]);
         }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    f32x16 nacc[2];
+    for (int u = u0; u < u1; u += 2) {
+        step(u, sacc, nacc);
+        if (u + 1 < u1) step(u + 1, nacc, sacc);
     }
     if (!active) return;
     const float l_tot = l_run + shx(l_run, 32), inv = a.NS > 1 ? 1.f : l_tot == 0.f ? 0.f : 1.f / l_tot;
@@ -991,7 +1159,7 @@ __global__ __launch_bounds__(512) void k_kv8_merge(const Kv8Attn a) {
     if (rt * 32 >= (a.s.cu[b + 1] - a.s.cu[b]) * a.G) return;
     const Kv8Row r = kv8_row(a, b, kvh, rt * 32 + (lane & 31));
     float o[8];
-    kv8_sum<HD, false>(a.part + (size_t)((b * a.rts + rt) * a.Hkv + kvh) * a.NS * AttnPartial<HD>::FLOATS, a.NS, w >> 1, w & 1, lane, a.m_init, a.scale_log2e, o);
+    kv8_sum<HD>(a.part + (size_t)((b * a.rts + rt) * a.Hkv + kvh) * a.NS * AttnPartial<HD>::FLOATS, a.NS, w >> 1, w & 1, lane, a.m_init, a.scale_log2e, o);
     kv8_store<HD, SRC>(a, r, w >> 1, w & 1, o, lane);
 }
 

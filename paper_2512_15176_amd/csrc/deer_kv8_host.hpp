@@ -146,21 +146,41 @@ hipError_t kv8_append(Kv8Cache &c, hipStream_t s, int layer, const T *k, const T
            : c.p.head_dim == 64 ? kv8_append_hd<64>(c, s, layer, k, v, k_stride, v_stride) : kv8_append_hd<32>(c, s, layer, k, v, k_stride, v_stride);
 }
 
+// What an attention launch takes, in microseconds, by what it streams: tiles x pages, of 16 packed rows (k_kv8_attn_few) or of 4 x 32
+// (k_kv8_attn_many, with its merge).  Fitted to the heads of the 4B / 8B models and the drafter, 1 to 16 sequences, 1 to 128 rows;
+// good to about 25 %.  few / many measured, heads 32 / 8 of 128: 1 sequence, 32 rows behind 500, 4095, 16000 and 30000 tokens 9.3 / 18.5,
+// 16.2 / 20.8, 30 / 40, 48 / 49; 4 behind 8000 48 / 39; 16 behind 1000 29 / 32, behind 16000 326 / 196; 16 behind 16000 with 8 and
+// 12 rows 128 / 139 and 201 / 165; 8 prompts of 100 20.6 / 11.7.  Heads 14 / 2 of 64: 7 sequences, 31 rows behind 3000 15.8 / 21.8;
+// 16, 32 rows behind 8000 46 / 40.
+struct Kv8Shares { long long items; int NS; };
+inline Kv8Shares kv8_shares(long long items, long long tiles, int pages) {
+    // key ranges: as many as fill the chip (two workgroups of four waves per compute unit), each with eight pages or its waves' four
+    return Kv8Shares{items, (int)std::max<long long>(1, std::min<long long>({KV8_WGS / std::max<long long>(items, 1), KV8_PART_TILES / std::max<long long>(tiles, 1), 64, (pages + 7) / 8}))};
+}
+inline double kv8_few_us(const Kv8Shares &s, int pages, int hd) { return 6.0 + 0.008 * (double)s.items * s.NS + 0.0012 * (double)s.items * pages * hd / 128; }
+inline double kv8_many_us(const Kv8Shares &s, int pages, int hd) { return 12.0 + 0.005 * (double)s.items * pages * hd / 128 + (s.NS > 1 ? 5.0 + 0.2 * s.NS : 0.0); }
+// A pool beyond the memory-side cache (256 MB) is streamed past the L2 where a page has one reader: 16 x 32768 tokens of 8 heads
+// of 128 206 -> 186 us, but 16 x 4096, which that cache holds from pass to pass of one layer, 31 -> 34.
+constexpr double KV8_STREAM_BYTES = 256e6;
+
 template <int HD, int SRC>
 hipError_t kv8_attend_src(Kv8Cache &c, hipStream_t s, Kv8Attn &a) {
     const int B = c.batch, packed = c.max_new * a.G, pages = (c.max_len + KV8_PAGE - 1) / KV8_PAGE;
-    a.rts = (packed + 31) / 32;
-    const bool few = packed <= 32;
-    const int ty = few ? a.rts : (a.rts + 3) / 4;
-    const long long items = (long long)B * ty * a.Hkv, tiles = (long long)B * a.rts * a.Hkv;
-    // key ranges: as many as fill the chip (one workgroup of eight waves per compute unit, or two of four), each with work for its waves
-    const long long fill = (few ? KV8_WGS / 2 : KV8_WGS) / std::max<long long>(items, 1);
-    a.NS = (int)std::max<long long>(1, std::min<long long>({fill, KV8_PART_TILES / tiles, 64, few ? (pages + 7) / 8 : std::max(1, pages / 4)}));
-    const dim3 grid(a.Hkv * a.NS, ty, B);
-    if (few) hipLaunchKernelGGL((k_kv8_attn_few<HD, SRC>), grid, dim3(512), 0, s, a);
-    else hipLaunchKernelGGL((k_kv8_attn_many<HD, SRC>), grid, dim3(256), 0, s, a);
+    const int rt16 = (packed + 15) / 16, rt32 = (packed + 31) / 32, groups = (rt32 + 3) / 4;
+    const long long heads = (long long)B * a.Hkv;
+    const Kv8Shares f = kv8_shares(heads * rt16, heads * rt16, pages);
+    Kv8Shares m = kv8_shares(heads * groups, heads * rt32, pages * 2);      // (a workgroup of this kernel takes four pages at least)
+    if (kv8_few_us(f, pages, HD) <= kv8_many_us(m, pages, HD) && rt16 <= 65535) {
+        a.rts = rt16; a.NS = f.NS;
+        const dim3 grid(a.Hkv * a.NS, rt16, B);
+        if (rt16 == 1 && (double)c.p.n_layers * B * pages * c.page_bytes() > KV8_STREAM_BYTES) hipLaunchKernelGGL((k_kv8_attn_few<HD, SRC, true>), grid, dim3(256), 0, s, a);
+        else hipLaunchKernelGGL((k_kv8_attn_few<HD, SRC, false>), grid, dim3(256), 0, s, a);
+        return hipGetLastError();
+    }
+    a.rts = rt32; a.NS = m.NS;
+    hipLaunchKernelGGL((k_kv8_attn_many<HD, SRC>), dim3(a.Hkv * a.NS, groups, B), dim3(256), 0, s, a);
     if (hipError_t e = hipGetLastError()) return e;
-    if (!few && a.NS > 1) hipLaunchKernelGGL((k_kv8_merge<HD, SRC>), dim3(a.Hkv, a.rts, B), dim3(4 * HD), 0, s, a);
+    if (a.NS > 1) hipLaunchKernelGGL((k_kv8_merge<HD, SRC>), dim3(a.Hkv, rt32, B), dim3(4 * HD), 0, s, a);
     return hipGetLastError();
 }
 // a: what the caller knows (limits, q, out or fragments)

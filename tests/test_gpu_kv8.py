@@ -212,6 +212,7 @@ def test_attention(heads, dtype, start, new):
     p.attend(limits=every)                                   # all see all
     p.attend(limits=[int(p.rng.integers(-2, e + 3)) for e in every], scale=0.3)   # any number of keys, none among them
     p.attend(limits=[0] * len(every))
+    p.attend(limits=[0 if i % 3 == 1 else e for i, e in enumerate(every)])      # rows that see nothing among rows that see all
     p.kv.close()
 
 
