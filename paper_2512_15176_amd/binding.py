@@ -374,6 +374,10 @@ class Kv8Cache:
             raise RuntimeError("Kv8Cache needs a GPU: libdeer has no CPU path")
         self.device = torch.device("cuda", device)
         self.stream = torch.cuda.current_stream(self.device)
+        self._stream = self.stream.cuda_stream
+        # the current stream's handle: without the Stream object that torch.cuda.current_stream makes (2 us of a call's 9)
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        self._current = (lambda: raw(device)) if raw else (lambda: torch.cuda.current_stream(self.device).cuda_stream)
         self.n_layers, self.n_q_heads, self.n_kv_heads, self.head_dim = n_layers, n_q_heads, n_kv_heads, head_dim
         self.max_batch, self.max_seq = max_batch, max_seq
         self.max_rows = 64 * max_batch if max_rows is None else max_rows
@@ -411,15 +415,17 @@ class Kv8Cache:
         """One call on the cache's stream, ordered with the current one."""
         if self.ctx is None:
             raise RuntimeError("the cache is closed")
-        cur = self.torch.cuda.current_stream(self.device)
-        other = cur.cuda_stream != self.stream.cuda_stream
-        if other:
+        if self._current() == self._stream:
+            rc = fn(self.ctx, *args)
+        else:
+            cur = self.torch.cuda.current_stream(self.device)
             self.stream.wait_stream(cur)
             for t in tensors:
                 t.record_stream(self.stream)
-        self._check(fn(self.ctx, *args))
-        if other:
+            rc = fn(self.ctx, *args)
             cur.wait_stream(self.stream)
+        if rc:
+            self._check(rc)
 
     def _ints(self, x, n, what):
         if x.device != self.device or x.dtype != self.torch.int32 or not x.is_contiguous() or x.numel() != n:
@@ -428,14 +434,14 @@ class Kv8Cache:
 
     def _rows_of(self, x, heads, what):
         """The row stride of x [rows][heads][head_dim]; heads and channels are dense."""
-        if x.device != self.device or x.dim() != 3 or tuple(x.shape) != (self.rows, heads, self.head_dim):
+        if x.device != self.device or x.shape != (self.rows, heads, self.head_dim):
             raise ValueError(f"{what} must be [{self.rows}][{heads}][{self.head_dim}] on {self.device}")
         if x.dtype not in (self.torch.float32, self.torch.bfloat16):
             raise TypeError(f"{what} must be float32 or bfloat16")
-        width = heads * self.head_dim
-        if self.rows and (x.stride(2) != 1 or (heads > 1 and x.stride(1) != self.head_dim)):
+        row, head, one = x.stride()
+        if self.rows and (one != 1 or (heads > 1 and head != self.head_dim)):
             raise ValueError(f"{what}: a row's heads must be dense")
-        return x.stride(0) if self.rows > 1 else width
+        return row if self.rows > 1 else heads * self.head_dim
 
     def _dtype(self, x):
         return DEER_F32 if x.dtype == self.torch.float32 else DEER_BF16

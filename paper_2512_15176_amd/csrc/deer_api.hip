@@ -1817,18 +1817,10 @@ int deer_kv8_read(deer_kv8 *c, int32_t layer, const int32_t *seq_dev, const int3
     if (n == 0) return DEER_OK;
     if (!seq_dev || !pos_dev || !k_dev || !v_dev || !aligned4(seq_dev) || !aligned4(pos_dev) || !aligned16(k_dev) || !aligned16(v_dev))
         return fail8(c, DEER_EINVAL, "null or unaligned pointer");
-    const size_t items = (size_t)n * (p.head_dim / 8);
     DeviceScope dev(c->device);
     KV8CHK(c, dev.err);
-    const dim3 grid((unsigned)((items + 255) / 256), p.n_kv_heads);
-    const Kv8Hot ring = c->c.ring_view(layer);
-    if (dtype == DEER_F32)
-        hipLaunchKernelGGL(k_kv8_read<float>, grid, dim3(256), 0, c->stream, c->c.st, seq_dev, pos_dev, n, ring, c->c.layer_pages(layer), c->c.layer_scales(layer),
-                           p.n_kv_heads, p.head_dim, (float *)k_dev, (float *)v_dev);
-    else
-        hipLaunchKernelGGL(k_kv8_read<uint16_t>, grid, dim3(256), 0, c->stream, c->c.st, seq_dev, pos_dev, n, ring, c->c.layer_pages(layer), c->c.layer_scales(layer),
-                           p.n_kv_heads, p.head_dim, (uint16_t *)k_dev, (uint16_t *)v_dev);
-    KV8CHK(c, hipGetLastError());
+    if (dtype == DEER_F32) KV8CHK(c, kv8_read(c->c, c->stream, layer, seq_dev, pos_dev, n, (float *)k_dev, (float *)v_dev));
+    else KV8CHK(c, kv8_read(c->c, c->stream, layer, seq_dev, pos_dev, n, (uint16_t *)k_dev, (uint16_t *)v_dev));
     return DEER_OK;
 }
 

@@ -49,19 +49,23 @@ struct Kv8Hot {        // bf16 rows of one layer
 // ------------------------------------------------------------------------------------------
 // tables of a pass
 // ------------------------------------------------------------------------------------------
-__device__ __forceinline__ int kv8_scan(int v, int *tmp) {   // inclusive sum over 1024 threads; tmp: 16 words of LDS
+// Inclusive sums of two pairs of numbers (each below 2^31) over 1024 threads, in one pass; tmp: LDS
+struct Kv8Sums { unsigned long long a, b; };
+__device__ __forceinline__ unsigned long long kv8_up(unsigned long long v, int off, int lane) {
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_ds_bpermute((lane - off) << 2, (int)(uint32_t)v);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_ds_bpermute((lane - off) << 2, (int)(uint32_t)(v >> 32));
+    return lane >= off ? ((unsigned long long)hi << 32) | lo : 0ull;
+}
+__device__ __forceinline__ Kv8Sums kv8_scan(Kv8Sums v, Kv8Sums (&tmp)[16]) {
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
 #pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-        const int o = __builtin_amdgcn_ds_bpermute((lane - off) << 2, v);
-        if (lane >= off) v += o;
-    }
+    for (int off = 1; off < 64; off <<= 1) { v.a += kv8_up(v.a, off, lane); v.b += kv8_up(v.b, off, lane); }
     if (lane == 63) tmp[w] = v;
     __syncthreads();
-    int base = 0;
-    for (int i = 0; i < w; ++i) base += tmp[i];
-    __syncthreads();
-    return v + base;
+#pragma unroll
+    for (int i = 0; i < 15; ++i)
+        if (i < w) { v.a += tmp[i].a; v.b += tmp[i].b; }
+    return v;
 }
 
 // number of entries of the ascending a[0 .. n) that are <= x
@@ -86,12 +90,14 @@ __global__ void k_kv8_init(Kv8State s) {
 // table: taken page i is the i-th page given back (in order of sequence and block), then the stack's top and down.
 // A sequence is refused (keeps its pages and tokens, gets no rows) for numbers out of range, a start behind its tokens, a start
 // inside a page whose bf16 rows are gone, or, like every growing one behind it, where the pages do not suffice.
-// Every workgroup works out all sequences (a few microseconds of scans, once for the launch) and writes its share of table entries
-// and rows; the state itself is written by the last to arrive, when all have read it.  grid: any; 1024 threads; B <= 1024.
+// Every workgroup works out all sequences (one scan) and writes its share of table entries and rows, four rows to a thread; the
+// state itself is written by the last to arrive, when all have read it.  Bound by latency: 16 sequences 4 us, 1000 prompts with
+// 512500 rows 9 us (their 6.1 MB would take 1).  grid: any; 1024 threads; B <= 1024.
 __global__ __launch_bounds__(1024) void k_kv8_reserve(Kv8State s, const int *__restrict__ start, int start_add, const int *__restrict__ count,
                                                       int count_const, int B, int rows, int max_new, int max_len, int scratch) {
     __shared__ int s_row[KV8_MAX_BATCH], s_start[KV8_MAX_BATCH], s_n[KV8_MAX_BATCH], s_held[KV8_MAX_BATCH], s_tp[KV8_MAX_BATCH],
-        s_grow[KV8_MAX_BATCH], s_give[KV8_MAX_BATCH], tmp[16], s_taken, s_refused, s_flag;
+        s_grow[KV8_MAX_BATCH], s_give[KV8_MAX_BATCH], s_taken, s_given, s_refused, s_flag;
+    __shared__ Kv8Sums tmp[16];
     const int b = threadIdx.x;
     int st = 0, n = 0, len = 0, held = 0, hot = 0, base = 0;
     if (b < B) {
@@ -100,23 +106,23 @@ __global__ __launch_bounds__(1024) void k_kv8_reserve(Kv8State s, const int *__r
         len = s.len[b]; held = s.held[b]; hot = s.hot[b]; base = s.base[b];
     }
     const int top = s.stat[0];
-    if (b == 0) { s_taken = 0; s_refused = 0; }
-    const int rn = min(max(n, 0), rows);              // the rows' layout follows the request, granted or not
-    const int row_end = kv8_scan(b < B ? rn : 0, tmp), row0 = row_end - (b < B ? rn : 0);
+    if (b == 0) { s_taken = 0; s_given = 0; s_refused = 0; }
+    const int rn = b < B ? min(max(n, 0), rows) : 0;              // the rows' layout follows the request, granted or not
     const bool in_ring = st / KV8_PAGE >= hot, kept = st / KV8_PAGE == base / KV8_PAGE && st <= base;
-    bool ok = b < B && st >= 0 && n >= 0 && n <= max_new && st <= max_len && st + n <= max_len && st <= len &&
-              ((st & (KV8_PAGE - 1)) == 0 || in_ring || kept) && row_end <= rows;
-    const int tp = ok ? (st + n + KV8_PAGE - 1) / KV8_PAGE : held;
-    const int grow = max(0, tp - held), give = max(0, held - tp);
-    const int grow_end = kv8_scan(grow, tmp), give_end = kv8_scan(give, tmp);
-    if (b < KV8_MAX_BATCH) { s_give[b] = give_end; s_grow[b] = grow_end; }
+    bool ok = b < B && st >= 0 && n >= 0 && n <= max_new && st <= max_len && st + n <= max_len && st <= len && ((st & (KV8_PAGE - 1)) == 0 || in_ring || kept);
+    const int tp = ok ? (st + n + KV8_PAGE - 1) / KV8_PAGE : held, first = st / KV8_PAGE;
+    const int grow = max(0, tp - held), give = max(0, held - tp), touched = ok && n > 0 ? (st + n - 1) / KV8_PAGE - first + 1 : 0;
+    const Kv8Sums v = kv8_scan(Kv8Sums{((unsigned long long)rn << 32) | (unsigned)touched, ((unsigned long long)grow << 32) | (unsigned)give}, tmp);
+    const int row_end = (int)(v.a >> 32), row0 = row_end - rn, touched_end = (int)(uint32_t)v.a, grow_end = (int)(v.b >> 32), give_end = (int)(uint32_t)v.b;
+    // A sequence whose rows end behind the last is refused, and so is every one behind it: what they would give or take lies behind
+    // everybody's in the sums, and counts for nobody.
+    ok = ok && row_end <= rows;
+    if (ok) atomicMax(&s_given, give_end);
     __syncthreads();
-    const int given = s_give[KV8_MAX_BATCH - 1], avail = top + given;
+    const int given = s_given, avail = top + given;
     if (grow > 0 && grow_end > avail) ok = false;
-    const int m = ok ? n : 0, first = st / KV8_PAGE, last = (st + max(m, 1) - 1) / KV8_PAGE;
-    const int touched = m > 0 ? last - first + 1 : 0;
-    const int touched_end = kv8_scan(touched, tmp);
-    s_row[b] = b < B ? row0 : 0x7fffffff; s_start[b] = st; s_n[b] = m; s_held[b] = held; s_tp[b] = tp;
+    const int m = ok ? n : 0, last = (st + max(m, 1) - 1) / KV8_PAGE;
+    s_row[b] = b < B ? row0 : 0x7fffffff; s_start[b] = st; s_n[b] = m; s_held[b] = held; s_tp[b] = tp; s_grow[b] = grow_end; s_give[b] = give_end;
     if (ok && grow > 0) atomicMax(&s_taken, grow_end);
     if (b < B && !ok) atomicAdd(&s_refused, 1);
     __syncthreads();
@@ -127,23 +133,38 @@ __global__ __launch_bounds__(1024) void k_kv8_reserve(Kv8State s, const int *__r
     };
     auto take = [&](int i) { return i < given ? back(i) : s.free[top - 1 - (i - given)]; };
     const int tid = blockIdx.x * 1024 + threadIdx.x, nth = gridDim.x * 1024;
-    for (int i = tid; i < taken; i += nth) {
-        const int q = kv8_upper(s_grow, KV8_MAX_BATCH, i);
-        s.table[(size_t)q * s.max_blocks + s_held[q] + i - (q ? s_grow[q - 1] : 0)] = take(i);
-    }
-    for (int r = tid; r < rows; r += nth) {
-        const int q = kv8_upper(s_row, B, r) - 1;
-        int sl = -1, sq = -1, ps = 0;
-        if (q >= 0 && r - s_row[q] < s_n[q]) {
-            ps = s_start[q] + r - s_row[q]; sq = q;
-            const int pi = ps / KV8_PAGE;
-            const int page = pi < s_held[q] ? s.table[(size_t)q * s.max_blocks + pi] : take((q ? s_grow[q - 1] : 0) + pi - s_held[q]);
-            sl = page * KV8_PAGE + ps % KV8_PAGE;
+    for (int r0 = tid * 4; r0 < rows; r0 += nth * 4) {
+        int q = kv8_upper(s_row, B, r0) - 1, at = -1, page = 0;      // at: the table entry that `page` is
+        int sl[4], sq[4], ps[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int r = r0 + e;
+            while (q + 1 < B && s_row[q + 1] <= r) ++q;
+            sl[e] = sq[e] = -1; ps[e] = 0;
+            if (q >= 0 && r - s_row[q] < s_n[q]) {
+                ps[e] = s_start[q] + r - s_row[q]; sq[e] = q;
+                const int pi = ps[e] / KV8_PAGE, entry = q * s.max_blocks + pi;      // (fits: 1024 sequences of 2^14 pages)
+                if (entry != at) {
+                    at = entry;
+                    page = pi < s_held[q] ? s.table[entry] : take((q ? s_grow[q - 1] : 0) + pi - s_held[q]);
+                }
+                if (ps[e] % KV8_PAGE == 0 && pi >= s_held[q]) s.table[entry] = page;      // (a page that is taken starts with a row of the pass)
+                sl[e] = page * KV8_PAGE + ps[e] % KV8_PAGE;
+            }
         }
-        s.slot[r] = sl; s.row_seq[r] = sq; s.row_pos[r] = ps;
+        if (r0 + 4 <= rows) {
+            *(int4 *)(s.slot + r0) = make_int4(sl[0], sl[1], sl[2], sl[3]);
+            *(int4 *)(s.row_seq + r0) = make_int4(sq[0], sq[1], sq[2], sq[3]);
+            *(int4 *)(s.row_pos + r0) = make_int4(ps[0], ps[1], ps[2], ps[3]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 3; ++e)
+                if (r0 + e < rows) { s.slot[r0 + e] = sl[e]; s.row_seq[r0 + e] = sq[e]; s.row_pos[r0 + e] = ps[e]; }
+        }
     }
     for (int j = tid; j < given - taken; j += nth) s.free[top + j] = back(given - 1 - j);   // entries from `top` on: read by nobody here
-    if (!arrive_last(&s.stat[2], gridDim.x, &s_flag)) return;
+    if (gridDim.x > 1) { if (!arrive_last(&s.stat[2], gridDim.x, &s_flag)) return; }
+    else __syncthreads();
     if (b < B) {
         s.start[b] = st; s.count[b] = m; s.cu[b] = min(row0, rows);
         s.hotbase[b] = scratch ? (touched_end - touched - first) * KV8_PAGE : 0;
@@ -233,42 +254,34 @@ __device__ __forceinline__ uint2 quant8(uint4 v, float inv) {
     }
     return make_uint2((uint32_t)o[0], (uint32_t)o[1]);
 }
-// A page's 64 rows of one head in registers, K and V in fragment order: thread t has the lanes' vectors of chunks t, t + 256, .. (two
-// fragments each).  They are quantised into the pool; 256 threads, all of which call it.
+// A page's 64 rows of one head in registers, K and V in fragment order: thread t of 4 HD has the two fragments' vectors of chunk t / 64
+// that belong to lane t % 64.  They are quantised into the pool; all threads call it.
 template <int HD>
-struct Kv8Regs {
-    static constexpr int NC = KV8_PAGE * HD / 16;   // chunk lanes of K, and of V
-    static constexpr int PER = (NC + 255) / 256;
-    uint4 x[2][PER][2];
-};
-template <int HD>
-__device__ __forceinline__ void kv8_quantise(const Kv8Regs<HD> &p, uint8_t *__restrict__ pp, float *__restrict__ scales, float (&s_max)[2][4]) {
-    using R = Kv8Regs<HD>;
-    float amax[2] = {0.f, 0.f};
+__device__ __forceinline__ void kv8_quantise(const uint4 (&x)[2][2], uint8_t *__restrict__ pp, float *__restrict__ scales, float (&s_max)[2][HD / 16]) {
+    constexpr int W = HD / 16;      // waves
+    float amax[2];
 #pragma unroll
     for (int kv = 0; kv < 2; ++kv) {
-#pragma unroll
-        for (int i = 0; i < R::PER; ++i) {
-            if (R::NC % 256 && threadIdx.x + 256 * i >= R::NC) continue;
-            amax[kv] = amax8(amax8(amax[kv], p.x[kv][i][0]), p.x[kv][i][1]);
-        }
-#pragma unroll
-        for (int off = 1; off < 64; off <<= 1) amax[kv] = fmaxf(amax[kv], shx(amax[kv], off));
+        amax[kv] = amax8(amax8(0.f, x[kv][0]), x[kv][1]);
+        amax[kv] = fmaxf(amax[kv], dppf<0xB1>(amax[kv]));      // (see dpp: sixteen lanes, then the four groups)
+        amax[kv] = fmaxf(amax[kv], dppf<0x4E>(amax[kv]));
+        amax[kv] = fmaxf(amax[kv], dppf<0x141>(amax[kv]));
+        amax[kv] = fmaxf(amax[kv], dppf<0x140>(amax[kv]));
+        amax[kv] = fmaxf(amax[kv], shx(amax[kv], 16));
+        amax[kv] = fmaxf(amax[kv], shx(amax[kv], 32));
         if ((threadIdx.x & 63) == 0) s_max[kv][threadIdx.x >> 6] = amax[kv];
     }
     __syncthreads();
 #pragma unroll
     for (int kv = 0; kv < 2; ++kv) {
-        const float sc = kv8_scale(fmaxf(fmaxf(s_max[kv][0], s_max[kv][1]), fmaxf(s_max[kv][2], s_max[kv][3])));
+        float m = s_max[kv][0];
+#pragma unroll
+        for (int i = 1; i < W; ++i) m = fmaxf(m, s_max[kv][i]);
+        const float sc = kv8_scale(m);
         const float inv = __uint_as_float((254u << 23) - __float_as_uint(sc));    // 1 / 2^e
         if (threadIdx.x == 0) scales[kv] = sc;
-#pragma unroll
-        for (int i = 0; i < R::PER; ++i) {
-            const int c = threadIdx.x + 256 * i;
-            if (R::NC % 256 && c >= R::NC) continue;
-            const uint2 a = quant8(p.x[kv][i][0], inv), d = quant8(p.x[kv][i][1], inv);
-            *(uint4 *)(pp + (size_t)kv * KV8_PAGE * HD + (size_t)c * 16) = make_uint4(a.x, a.y, d.x, d.y);
-        }
+        const uint2 a = quant8(x[kv][0], inv), d = quant8(x[kv][1], inv);
+        *(uint4 *)(pp + (size_t)kv * KV8_PAGE * HD + (size_t)threadIdx.x * 16) = make_uint4(a.x, a.y, d.x, d.y);
     }
 }
 
@@ -299,15 +312,16 @@ __global__ __launch_bounds__(256) void k_kv8_keep(Kv8State s, Kv8Hot ring) {
 // and the page one of its last two, and, quantised, to the pool if the page is complete.
 // A token with an infinity or NaN in its K or V row of a head gets a key of NaNs and a value of zeros there: rows that see it come out
 // NaN, and rows that do not, whose weight for it is zero, do not meet 0 x NaN.
-// grid: x page of the sequence's pass, y kv head, z sequence; 256 threads
+// Bound by latency: everything that is read is asked for before anything is waited for (16 sequences x 32 rows, 8 heads of 128:
+// 9 us, the launch's 2 and 7 for tables, rows, LDS and stores; a prompt of 4096 rows, 42 MB, 15 us).
+// grid: x page of the sequence's pass, y kv head, z sequence; 4 HD threads
 template <int HD, typename SrcT>
-__global__ __launch_bounds__(256) void k_kv8_append(Kv8State s, const SrcT *__restrict__ k, const SrcT *__restrict__ v, size_t k_stride, size_t v_stride,
-                                                    Kv8Hot hot, Kv8Hot ring, int is_long, uint8_t *__restrict__ pages, float *__restrict__ scales, int Hkv) {
-    using R = Kv8Regs<HD>;
+__global__ __launch_bounds__(4 * HD) void k_kv8_append(Kv8State s, const SrcT *__restrict__ k, const SrcT *__restrict__ v, size_t k_stride, size_t v_stride,
+                                                       Kv8Hot hot, Kv8Hot ring, int is_long, uint8_t *__restrict__ pages, float *__restrict__ scales, int Hkv) {
     constexpr int OCTS = HD / 8, VS = HD + 8;       // padded row of V in LDS
     __shared__ __attribute__((aligned(16))) uint16_t s_v[KV8_PAGE * VS];
     __shared__ int s_bad[KV8_PAGE];
-    __shared__ float s_max[2][4];
+    __shared__ float s_max[2][HD / 16];
     const int b = blockIdx.z, head = blockIdx.y, n = s.count[b];
     if (n == 0) return;
     const int st = s.start[b], end = st + n, first = st / KV8_PAGE, last = (end - 1) / KV8_PAGE, page = first + blockIdx.x;
@@ -318,81 +332,76 @@ __global__ __launch_bounds__(256) void k_kv8_append(Kv8State s, const SrcT *__re
     const int carry = t0 > 0 ? s.carry[b] : 0;             // (0: the older rows are where they belong)
     const Kv8At at = kv8_at(s, hot, ring, b, head, page, HD);
     const size_t older = carry ? at.kept : at.ring;        // carry: the pass is long (kept by k_kv8_keep), or taken back
-    for (int i = threadIdx.x; i < KV8_PAGE; i += 256) s_bad[i] = 0;
-    __syncthreads();
-    for (int i = threadIdx.x; i < KV8_PAGE * OCTS; i += 256) {
-        const int tok = i / OCTS, oct = i % OCTS;
-        if (tok < t0 || tok >= t1) continue;
-        const uint4 x = load8_bf16(v + (size_t)(row0 + tok) * v_stride + (size_t)head * HD + oct * 8);
-        if (nonfinite8(x)) s_bad[tok] = 1;
-        *(uint4 *)(s_v + tok * VS + oct * 8) = x;
+    const int id = whole ? s.table[(size_t)b * s.max_blocks + page] : -1;
+    // V: the rows' octets, two to a thread
+    uint4 xv[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int tok = (threadIdx.x + 4 * HD * i) / OCTS, oct = threadIdx.x % OCTS;
+        xv[i] = make_uint4(0u, 0u, 0u, 0u);
+        if (tok >= t0 && tok < t1) xv[i] = load8_bf16(v + (size_t)(row0 + tok) * v_stride + (size_t)head * HD + oct * 8);
     }
-    R p;
+    // K in fragment order, and what is older of V's fragments
+    const int lane = threadIdx.x & 63, f0 = (threadIdx.x >> 6) * 2, rr = lane & 31, half = lane >> 5, blk = f0 / (HD / 16) * 32;
+    const int tok = blk + 16 * ((rr >> 2) & 1) + 4 * (rr >> 3) + (rr & 3);      // of a K vector
+    const bool mine = tok >= t0 && tok < t1, before = tok < t0;
+    uint4 x[2][2];
 #pragma unroll
-    for (int i = 0; i < R::PER; ++i) {
-        const int c = threadIdx.x + 256 * i, lane = c & 63, rr = lane & 31;
-        if (R::NC % 256 && c >= R::NC) continue;
+    for (int u = 0; u < 2; ++u) {
+        const int f = f0 + u, oct = f % (HD / 16) * 2 + half, tok0 = blk + 16 * half + 8 * u;     // tok0: the first of a V vector's eight tokens
+        const size_t off = ((size_t)f * 64 + lane) * 8;
+        x[0][u] = x[1][u] = make_uint4(0u, 0u, 0u, 0u);
+        if (mine) x[0][u] = load8_bf16(k + (size_t)(row0 + tok) * k_stride + (size_t)head * HD + oct * 8);
+        else if (before && (whole || carry)) x[0][u] = *(const uint4 *)(ring.k + older + off);
+        if (tok0 < t0 && (tok0 + 8 > t0 || whole || carry)) x[1][u] = *(const uint4 *)(ring.v + older + off);
+    }
+    if (threadIdx.x < KV8_PAGE) s_bad[threadIdx.x] = 0;
+    __syncthreads();
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const int f = (c >> 6) * 2 + u, tok = f / (HD / 16) * 32 + 16 * ((rr >> 2) & 1) + 4 * (rr >> 3) + (rr & 3), oct = f % (HD / 16) * 2 + (lane >> 5);
-            uint4 x = make_uint4(0u, 0u, 0u, 0u);
-            if (tok >= t0 && tok < t1) {
-                x = load8_bf16(k + (size_t)(row0 + tok) * k_stride + (size_t)head * HD + oct * 8);
-                if (nonfinite8(x)) s_bad[tok] = 1;
-            } else if (tok < t0 && (whole || carry)) x = *(const uint4 *)(ring.k + older + ((size_t)f * 64 + lane) * 8);
-            p.x[0][i][u] = x;
+    for (int i = 0; i < 2; ++i) {
+        const int vt = (threadIdx.x + 4 * HD * i) / OCTS, oct = threadIdx.x % OCTS;
+        if (nonfinite8(xv[i])) s_bad[vt] = 1;
+        *(uint4 *)(s_v + vt * VS + oct * 8) = xv[i];
+    }
+    if (mine && (nonfinite8(x[0][0]) || nonfinite8(x[0][1]))) s_bad[tok] = 1;
+    __syncthreads();
+    const bool bad = mine && s_bad[tok];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        const int f = f0 + u, ch = f % (HD / 16) / 2 * 32 + rr, tok0 = blk + 16 * half + 8 * u;
+        const size_t off = ((size_t)f * 64 + lane) * 8;
+        if (bad) x[0][u] = make_uint4(0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u);
+        if (mine || (before && carry)) {
+            *(uint4 *)(hot.k + at.hot + off) = x[0][u];
+            if (out) *(uint4 *)(ring.k + at.ring + off) = x[0][u];
         }
-    }
-    __syncthreads();
+        const bool some = tok0 < t1 && tok0 + 8 > t0;
+        if (some) {      // eight tokens of a channel
+            uint32_t w[4] = {x[1][u].x, x[1][u].y, x[1][u].z, x[1][u].w};
 #pragma unroll
-    for (int i = 0; i < R::PER; ++i) {
-        const int c = threadIdx.x + 256 * i, lane = c & 63, rr = lane & 31, half = lane >> 5;
-        if (R::NC % 256 && c >= R::NC) continue;
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const int f = (c >> 6) * 2 + u, blk = f / (HD / 16) * 32;
-            const size_t off = ((size_t)f * 64 + lane) * 8;
-            {
-                const int tok = blk + 16 * ((rr >> 2) & 1) + 4 * (rr >> 3) + (rr & 3);
-                const bool mine = tok >= t0 && tok < t1;
-                if (mine && s_bad[tok]) p.x[0][i][u] = make_uint4(0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u);
-                if (mine || (tok < t0 && carry)) *(uint4 *)(hot.k + at.hot + off) = p.x[0][i][u];
-                if (out && (mine || (tok < t0 && carry))) *(uint4 *)(ring.k + at.ring + off) = p.x[0][i][u];
+            for (int e = 0; e < 8; ++e) {
+                const int tk = tok0 + e;
+                const uint32_t y = tk >= t0 && tk < t1 && !s_bad[tk] ? s_v[tk * VS + ch] : tk < t0 ? (w[e >> 1] >> (16 * (e & 1))) & 0xffffu : 0u;
+                w[e >> 1] = e & 1 ? (w[e >> 1] & 0xffffu) | y << 16 : (w[e >> 1] & 0xffff0000u) | y;
             }
-            const int tok0 = blk + 16 * half + 8 * (f & 1), ch = f % (HD / 16) / 2 * 32 + rr;     // eight tokens of a channel
-            const bool some = tok0 < t1 && tok0 + 8 > t0, old = tok0 < t0;
-            uint4 x = make_uint4(0u, 0u, 0u, 0u);
-            if (old && (some || whole || carry)) x = *(const uint4 *)(ring.v + older + off);
-            if (some) {
-                uint32_t w[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int tok = tok0 + e;
-                    const uint32_t y = tok >= t0 && tok < t1 && !s_bad[tok] ? s_v[tok * VS + ch] : tok < t0 ? (w[e >> 1] >> (16 * (e & 1))) & 0xffffu : 0u;
-                    w[e >> 1] = e & 1 ? (w[e >> 1] & 0xffffu) | y << 16 : (w[e >> 1] & 0xffff0000u) | y;
-                }
-                x = make_uint4(w[0], w[1], w[2], w[3]);
-            }
-            if (some || (old && carry)) {
-                *(uint4 *)(hot.v + at.hot + off) = x;
-                if (out) *(uint4 *)(ring.v + at.ring + off) = x;
-            }
-            p.x[1][i][u] = x;
+            x[1][u] = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+        if (some || (tok0 < t0 && carry)) {
+            *(uint4 *)(hot.v + at.hot + off) = x[1][u];
+            if (out) *(uint4 *)(ring.v + at.ring + off) = x[1][u];
         }
     }
     if (!whole) return;      // (the whole workgroup)
-    const int id = s.table[(size_t)b * s.max_blocks + page];
     if ((unsigned)id >= (unsigned)s.n_pages) return;
     const size_t pg = (size_t)id * Hkv + head;
-    kv8_quantise<HD>(p, pages + pg * (2 * KV8_PAGE * HD), scales + pg * 2, s_max);
+    kv8_quantise<HD>(x, pages + pg * (2 * KV8_PAGE * HD), scales + pg * 2, s_max);
 }
 
 // Where another kernel has put the pass's rows into the hot pages (the engine's QKV projection): pages that they complete go to the pool,
 // and with the rows in the scratch (is_long) the last two pages to the ring.  grid as above
 template <int HD>
-__global__ __launch_bounds__(256) void k_kv8_settle(Kv8State s, Kv8Hot hot, Kv8Hot ring, int is_long, uint8_t *__restrict__ pages, float *__restrict__ scales, int Hkv) {
-    using R = Kv8Regs<HD>;
-    __shared__ float s_max[2][4];
+__global__ __launch_bounds__(4 * HD) void k_kv8_settle(Kv8State s, Kv8Hot hot, Kv8Hot ring, int is_long, uint8_t *__restrict__ pages, float *__restrict__ scales, int Hkv) {
+    __shared__ float s_max[2][HD / 16];
     const int b = blockIdx.z, head = blockIdx.y, n = s.count[b];
     if (n == 0) return;
     const int st = s.start[b], end = st + n, first = st / KV8_PAGE, last = (end - 1) / KV8_PAGE, page = first + blockIdx.x;
@@ -400,30 +409,26 @@ __global__ __launch_bounds__(256) void k_kv8_settle(Kv8State s, Kv8Hot hot, Kv8H
     const bool whole = end >= (page + 1) * KV8_PAGE, out = is_long && page >= last - 1;
     if (!whole && !out) return;
     const Kv8At at = kv8_at(s, hot, ring, b, head, page, HD);
-    R p;
+    const int id = whole ? s.table[(size_t)b * s.max_blocks + page] : -1;
+    uint4 x[2][2];
 #pragma unroll
     for (int kv = 0; kv < 2; ++kv)
 #pragma unroll
-        for (int i = 0; i < R::PER; ++i) {
-            const int c = threadIdx.x + 256 * i;
-            if (R::NC % 256 && c >= R::NC) continue;
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const size_t off = ((size_t)((c >> 6) * 2 + u) * 64 + (c & 63)) * 8;
-                p.x[kv][i][u] = *(const uint4 *)((kv ? hot.v : hot.k) + at.hot + off);
-                if (out) *(uint4 *)((kv ? ring.v : ring.k) + at.ring + off) = p.x[kv][i][u];
-            }
+        for (int u = 0; u < 2; ++u) {
+            const size_t off = ((size_t)((threadIdx.x >> 6) * 2 + u) * 64 + (threadIdx.x & 63)) * 8;
+            x[kv][u] = *(const uint4 *)((kv ? hot.v : hot.k) + at.hot + off);
+            if (out) *(uint4 *)((kv ? ring.v : ring.k) + at.ring + off) = x[kv][u];
         }
     if (!whole) return;
-    const int id = s.table[(size_t)b * s.max_blocks + page];
     if ((unsigned)id >= (unsigned)s.n_pages) return;
     const size_t pg = (size_t)id * Hkv + head;
-    kv8_quantise<HD>(p, pages + pg * (2 * KV8_PAGE * HD), scales + pg * 2, s_max);
+    kv8_quantise<HD>(x, pages + pg * (2 * KV8_PAGE * HD), scales + pg * 2, s_max);
 }
 
 // Rows as they stand in the cache (complete pages in 8 bits, else bf16) for n (sequence, position) pairs; zeros for a pair that names no
 // token.  One thread per (row, octet) of a head: the bytes of 16 tokens of a channel are one 16-byte vector, so that the tokens of a
-// workgroup, which mostly follow each other, find theirs in the lines that the first has fetched.  grid: x rows, y head
+// workgroup, which mostly follow each other, find theirs in the lines that the first has fetched.  (As vectors, turned in LDS, 4096
+// rows of 8 heads of 128 took as long, 13 us, and 512 rows in no order 20 instead of 5.)  grid: x rows, y head
 template <typename DstT>
 __global__ __launch_bounds__(256) void k_kv8_read(Kv8State s, const int *__restrict__ seq, const int *__restrict__ pos, int n, Kv8Hot ring,
                                                   const uint8_t *__restrict__ pages, const float *__restrict__ scales, int Hkv, int hd,

@@ -108,7 +108,7 @@ inline hipError_t kv8_reserve(Kv8Cache &c, hipStream_t s, const int *start, int 
     max_new = std::min(max_new, std::max(rows, 0));
     c.batch = batch; c.rows = rows; c.max_new = max_new; c.max_len = max_len;
     c.long_pass = max_new > KV8_PAGE;
-    const int wgs = std::max(1, std::min(64, (rows + 4095) / 4096));
+    const int wgs = std::max(1, std::min(256, (rows + 4095) / 4096));
     hipLaunchKernelGGL(k_kv8_reserve, dim3(wgs), dim3(1024), 0, s, c.st, start, start_add, count, count_const, batch, rows, max_new, max_len, c.long_pass ? 1 : 0);
     return hipGetLastError();
 }
@@ -118,7 +118,7 @@ inline unsigned kv8_touched(const Kv8Cache &c) { return (unsigned)(c.max_new + K
 
 template <int HD>
 hipError_t kv8_settle_hd(Kv8Cache &c, hipStream_t s, int layer) {
-    hipLaunchKernelGGL(k_kv8_settle<HD>, dim3(kv8_touched(c), c.p.n_kv_heads, c.batch), dim3(256), 0, s, c.st, c.hot_view(layer), c.ring_view(layer), c.long_pass ? 1 : 0,
+    hipLaunchKernelGGL(k_kv8_settle<HD>, dim3(kv8_touched(c), c.p.n_kv_heads, c.batch), dim3(4 * HD), 0, s, c.st, c.hot_view(layer), c.ring_view(layer), c.long_pass ? 1 : 0,
                        c.layer_pages(layer), c.layer_scales(layer), c.p.n_kv_heads);
     return hipGetLastError();
 }
@@ -135,7 +135,7 @@ hipError_t kv8_append_hd(Kv8Cache &c, hipStream_t s, int layer, const T *k, cons
         hipLaunchKernelGGL(k_kv8_keep<HD>, dim3(c.p.n_kv_heads, c.batch), dim3(256), 0, s, c.st, ring);
         if (hipError_t e = hipGetLastError()) return e;
     }
-    hipLaunchKernelGGL((k_kv8_append<HD, T>), dim3(kv8_touched(c), c.p.n_kv_heads, c.batch), dim3(256), 0, s, c.st, k, v, k_stride, v_stride, c.hot_view(layer), ring,
+    hipLaunchKernelGGL((k_kv8_append<HD, T>), dim3(kv8_touched(c), c.p.n_kv_heads, c.batch), dim3(4 * HD), 0, s, c.st, k, v, k_stride, v_stride, c.hot_view(layer), ring,
                        c.long_pass ? 1 : 0, c.layer_pages(layer), c.layer_scales(layer), c.p.n_kv_heads);
     return hipGetLastError();
 }
@@ -162,6 +162,14 @@ inline double kv8_many_us(const Kv8Shares &s, int pages, int hd) { return 12.0 +
 // A pool beyond the memory-side cache (256 MB) is streamed past the L2 where a page has one reader: 16 x 32768 tokens of 8 heads
 // of 128 206 -> 186 us, but 16 x 4096, which that cache holds from pass to pass of one layer, 31 -> 34.
 constexpr double KV8_STREAM_BYTES = 256e6;
+
+template <typename T>
+hipError_t kv8_read(const Kv8Cache &c, hipStream_t s, int layer, const int *seq, const int *pos, int n, T *k, T *v) {
+    const size_t items = (size_t)n * (c.p.head_dim / 8);
+    hipLaunchKernelGGL(k_kv8_read<T>, dim3((unsigned)((items + 255) / 256), c.p.n_kv_heads), dim3(256), 0, s, c.st, seq, pos, n, c.ring_view(layer), c.layer_pages(layer),
+                       c.layer_scales(layer), c.p.n_kv_heads, c.p.head_dim, k, v);
+    return hipGetLastError();
+}
 
 template <int HD, int SRC>
 hipError_t kv8_attend_src(Kv8Cache &c, hipStream_t s, Kv8Attn &a) {
