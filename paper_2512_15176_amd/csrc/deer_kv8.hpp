@@ -127,11 +127,11 @@ __global__ __launch_bounds__(1024) void k_kv8_reserve(Kv8State s, const int *__r
     if (b < B && !ok) atomicAdd(&s_refused, 1);
     __syncthreads();
     const int taken = s_taken;
-    auto back = [&](int i) {      // the i-th page given back
-        const int q = kv8_upper(s_give, KV8_MAX_BATCH, i), off = i - (q ? s_give[q - 1] : 0);
-        return s.table[(size_t)q * s.max_blocks + s_tp[q] + off];
+    auto back = [&](int i) {      // the table entry of the i-th page given back
+        const int q = kv8_upper(s_give, KV8_MAX_BATCH, i);
+        return s.table + (size_t)q * s.max_blocks + s_tp[q] + i - (q ? s_give[q - 1] : 0);
     };
-    auto take = [&](int i) { return i < given ? back(i) : s.free[top - 1 - (i - given)]; };
+    auto take = [&](int i) { return i < given ? *back(i) : s.free[top - 1 - (i - given)]; };
     const int tid = blockIdx.x * 1024 + threadIdx.x, nth = gridDim.x * 1024;
     for (int r0 = tid * 4; r0 < rows; r0 += nth * 4) {
         int q = kv8_upper(s_row, B, r0) - 1, at = -1, page = 0;      // at: the table entry that `page` is
@@ -162,7 +162,11 @@ __global__ __launch_bounds__(1024) void k_kv8_reserve(Kv8State s, const int *__r
                 if (r0 + e < rows) { s.slot[r0 + e] = sl[e]; s.row_seq[r0 + e] = sq[e]; s.row_pos[r0 + e] = ps[e]; }
         }
     }
-    for (int j = tid; j < given - taken; j += nth) s.free[top + j] = back(given - 1 - j);   // entries from `top` on: read by nobody here
+    for (int j = tid; j < given - taken; j += nth) {      // pages that nobody takes: their entries, and the stack's from `top` on, are read by nobody else
+        int *entry = back(given - 1 - j);
+        s.free[top + j] = *entry;
+        *entry = -1;
+    }
     if (gridDim.x > 1) { if (!arrive_last(&s.stat[2], gridDim.x, &s_flag)) return; }
     else __syncthreads();
     if (b < B) {
@@ -178,10 +182,7 @@ __global__ __launch_bounds__(1024) void k_kv8_reserve(Kv8State s, const int *__r
             s.base[b] = (scratch && older) || (kept && st % KV8_PAGE) ? st : st < base ? first * KV8_PAGE : base;
         }
     }
-    for (int i = b; i < given; i += 1024) {
-        const int q = kv8_upper(s_give, KV8_MAX_BATCH, i);
-        s.table[(size_t)q * s.max_blocks + s_tp[q] + i - (q ? s_give[q - 1] : 0)] = -1;
-    }
+    for (int i = b; i < min(given, taken); i += 1024) *back(i) = -1;
     if (b == 0) { s.stat[0] = top + given - taken; s.stat[1] = s_refused; }
 }
 

@@ -108,7 +108,9 @@ inline hipError_t kv8_reserve(Kv8Cache &c, hipStream_t s, const int *start, int 
     max_new = std::min(max_new, std::max(rows, 0));
     c.batch = batch; c.rows = rows; c.max_new = max_new; c.max_len = max_len;
     c.long_pass = max_new > KV8_PAGE;
-    const int wgs = std::max(1, std::min(256, (rows + 4095) / 4096));
+    // four rows to a thread; a call without rows only gives pages back, up to the batch's tables
+    const long long work = rows ? rows : std::min<long long>(c.p.n_pages, (long long)batch * c.st.max_blocks);
+    const int wgs = (int)std::max<long long>(1, std::min<long long>(256, (work + 4095) / 4096));
     hipLaunchKernelGGL(k_kv8_reserve, dim3(wgs), dim3(1024), 0, s, c.st, start, start_add, count, count_const, batch, rows, max_new, max_len, c.long_pass ? 1 : 0);
     return hipGetLastError();
 }
