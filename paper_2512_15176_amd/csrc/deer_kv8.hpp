@@ -584,23 +584,30 @@ __device__ __forceinline__ void kv8_load_q(const Kv8Attn &a, const Kv8Row &r, in
     }
 }
 
-// One step over 64 keys: scores (raw, of two tiles of 32 keys; the lane's keys are key0 + r and key0 + 32 + r) to weights, running
-// reference and sum, rescaled result.  First the reference: the largest score when it was last moved.  It moves where a score is more than
+// The reference of a step over 64 keys (raw scores of two tiles of 32 keys; the lane's keys are key0 + r and key0 + 32 + r), by which
+// sum and result are rescaled: the largest score when it was last moved.  It moves where a score is more than
 // 2^8 weights above it, not with every new maximum (of 32 rows one has a new maximum on almost every page of the first few thousand
 // keys): weights are then at most 2^8, as exact relative to each other as before.
 constexpr float KV8_SLACK = 8.f;      // log2 of the largest weight
-template <int HT>
-__device__ __forceinline__ void kv8_rescale(f32x16 (&sacc)[2], bool mask, int key0, int hi, float scale_log2e, float &m_run, float &l_run, f32x16 (&oacc)[HT]) {
-    if (mask) {
+// the larger of three (a NaN is passed over, as by fmaxf, whose operands are first made canonical: twice the instructions)
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+template <bool MASK, int HT>
+__device__ __forceinline__ void kv8_rescale(f32x16 (&sacc)[2], int key0, int hi, float scale_log2e, float &m_run, float &l_run, f32x16 (&oacc)[HT]) {
+    if (MASK) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
             if (key0 + r >= hi) sacc[0][r] = -INFINITY;
             if (key0 + 32 + r >= hi) sacc[1][r] = -INFINITY;
         }
     }
-    float mx = fmaxf(sacc[0][0], sacc[1][0]);
+    float m0 = max3(sacc[0][0], sacc[0][1], sacc[0][2]), m1 = max3(sacc[1][0], sacc[1][1], sacc[1][2]);
 #pragma unroll
-    for (int r = 1; r < 16; ++r) mx = fmaxf(mx, fmaxf(sacc[0][r], sacc[1][r]));
+    for (int r = 3; r < 15; r += 2) { m0 = max3(m0, sacc[0][r], sacc[0][r + 1]); m1 = max3(m1, sacc[1][r], sacc[1][r + 1]); }
+    const float mx = fmaxf(max3(m0, sacc[0][15], sacc[1][15]), m1);
     if (__builtin_amdgcn_ballot_w64((mx - m_run) * scale_log2e > KV8_SLACK)) {
         const float m_new = fmaxf(m_run, fmaxf(mx, shx(mx, 32)));
         const float alpha = __builtin_amdgcn_exp2f((m_run - m_new) * scale_log2e);
@@ -612,18 +619,6 @@ __device__ __forceinline__ void kv8_rescale(f32x16 (&sacc)[2], bool mask, int ke
             for (int r = 0; r < 16; ++r) oacc[tt][r] *= alpha;
     }
 }
-// .. then the weights.
-__device__ __forceinline__ void kv8_weights(f32x16 (&sacc)[2], float scale_log2e, float m_run, float &l_run) {
-    const float mb = m_run * scale_log2e;
-    float ls0 = 0.f, ls1 = 0.f;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-        sacc[0][r] = __builtin_amdgcn_exp2f(fmaf(sacc[0][r], scale_log2e, -mb)); ls0 += sacc[0][r];
-        sacc[1][r] = __builtin_amdgcn_exp2f(fmaf(sacc[1][r], scale_log2e, -mb)); ls1 += sacc[1][r];
-    }
-    l_run += ls0 + ls1;
-}
-
 // Registers 8 hh .. + 7 of O^T tile tt of a lane's row, normalised: channels 32 tt + 8 q + 4 half .. + 3, q = 2 hh, 2 hh + 1
 template <int HD, int SRC>
 __device__ __forceinline__ void kv8_store(const Kv8Attn &a, const Kv8Row &r, int tt, int hh, const float (&o)[8], int lane) {
@@ -1017,7 +1012,11 @@ __global__ __launch_bounds__(256, HD == 128 && SRC == KV8_F32 ? 1 : 2) void k_kv
     const int per = (n + a.NS - 1) / opaque_s(a.NS), u0 = split * per, u1 = min(n, u0 + per);
     const int *table = a.s.table + (size_t)b * a.s.max_blocks;
     int ask = kv8_ask(a.s, table, u0);
-    uint32_t live = 0;       // bit u % 32: page u exists
+    // Pages that all rows of the wave see whole (those that see anything) need no mask, and take a loop of their own: a mask on a
+    // branch costs copies of all scores on the other.  A page that does not exist (read as page 0) needs one.
+    bool gone = false;
+    for (int i = u0 + lane; i < min(n8, u1); i += 64) gone = gone || (unsigned)table[i] >= (unsigned)a.s.n_pages;
+    const int clear = __builtin_amdgcn_ballot_w64(gone) ? u0 : min(min(n8, u1), sp.min8 / KV8_PAGE);
     // what a wave holds of the page on its way: 8-bit chunks with their scale.  (A hot page, of which a workgroup has one or two, is
     // read when it is placed: registers for its fragments on their way would be missing in the products.)
     uint4 raw[LPW];
@@ -1027,7 +1026,6 @@ __global__ __launch_bounds__(256, HD == 128 && SRC == KV8_F32 ? 1 : 2) void k_kv
         if (u >= n8) return;
         const int id = kv8_page(a.s, ask);
         ask = kv8_ask(a.s, table, u + 1);
-        live = id >= 0 ? live | 1u << (u & 31) : live & ~(1u << (u & 31));
         const size_t at = (size_t)max(id, 0) * a.Hkv + kvh;      // (a page that does not exist is read as page 0 and masked)
         const uint4 *p = (const uint4 *)(a.pages + at * (2 * KV8_PAGE * HD)) + w * LPW * 64 + lane;
 #pragma unroll
@@ -1076,9 +1074,6 @@ __global__ __launch_bounds__(256, HD == 128 && SRC == KV8_F32 ? 1 : 2) void k_kv
 #pragma unroll
                 for (int p = 0; p < N; ++p) { sacc[0] = mfma32(k[g & 1][2 * s], q[p][2 * g + s], sacc[0]); sacc[1] = mfma32(k[g & 1][2 * s + 1], q[p][2 * g + s], sacc[1]); }
             beside(g);
-            __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
-#pragma unroll
-            for (int i = 0; i < 4 * N; ++i) { __builtin_amdgcn_sched_group_barrier(0x8, 1, 0); __builtin_amdgcn_sched_group_barrier(0x2, 24 / GK / N, 0); }
         }
         __builtin_amdgcn_sched_barrier(0);
     };
@@ -1092,15 +1087,19 @@ __global__ __launch_bounds__(256, HD == 128 && SRC == KV8_F32 ? 1 : 2) void k_kv
         __syncthreads();
         if (active) scores(sacc, u0, [](int) {});
     }
-    auto step = [&](int u, f32x16 (&sacc)[2], f32x16 (&nacc)[2]) {     // sacc: page u's scores; nacc: the next page's
+    auto step = [&](auto masked, int u, f32x16 (&sacc)[2], f32x16 (&nacc)[2]) {     // sacc: page u's scores; nacc: the next page's
         __syncthreads();      // page u + 1's keys and page u's values are in LDS; page u's keys and u - 1's values have been read
         if (u + ahead < u1) { place(u + ahead); if (u + ahead + 1 < u1) fetch(u + ahead + 1); }
         if (!active) return;
-        const bool cold = u < n8;
-        const int page = cold ? u : hmin + u - n8;
-        int hi = cold ? r.lim8 : (r.h0 < r.lim && r.h0 / KV8_PAGE == page ? r.lim : 0);
-        if (cold && !(live >> (u & 31) & 1)) hi = 0;
-        kv8_rescale<HT>(sacc, __builtin_amdgcn_ballot_w64(r.lim > 0 && (page + 1) * KV8_PAGE > hi) != 0, page * KV8_PAGE + 16 * half, hi, a.scale_log2e, m_run, l_run, oacc);
+        constexpr bool MASK = decltype(masked)::value;
+        int page = u, hi = 0;
+        if (MASK) {
+            const bool cold = u < n8;
+            page = cold ? u : hmin + u - n8;
+            hi = cold ? ((unsigned)__builtin_amdgcn_readfirstlane(table[u]) < (unsigned)a.s.n_pages ? r.lim8 : 0) : (r.h0 < r.lim && r.h0 / KV8_PAGE == page ? r.lim : 0);
+        }
+        kv8_rescale<MASK, HT>(sacc, page * KV8_PAGE + 16 * half, hi, a.scale_log2e, m_run, l_run, oacc);
+        __builtin_amdgcn_s_setprio(1);      // (the other workgroup's wave does its vector work meanwhile: 200 -> 190 us for a prompt of 4096)
         const float mb = m_run * a.scale_log2e;
         float ls[2] = {0.f, 0.f};
         scores(nacc, min(u + 1, u1 - 1), [&](int g) {       // the weights of page u, a share beside every group
@@ -1109,6 +1108,7 @@ __global__ __launch_bounds__(256, HD == 128 && SRC == KV8_F32 ? 1 : 2) void k_kv
 #pragma unroll
                 for (int j = 0; j < 2; ++j) { sacc[j][e] = __builtin_amdgcn_exp2f(fmaf(sacc[j][e], a.scale_log2e, -mb)); ls[j] += sacc[j][e]; }
         });
+        __builtin_amdgcn_s_setprio(0);
         l_run += ls[0] + ls[1];
         const uint4 *fr = buf[1][u & 1] + lane;
         uint4 v[2][HT];
@@ -1134,9 +1134,14 @@ __global__ __launch_bounds__(256, HD == 128 && SRC == KV8_F32 ? 1 : 2) void k_kv
         __builtin_amdgcn_sched_barrier(0);
     };
     f32x16 nacc[2];
-    for (int u = u0; u < u1; u += 2) {
-        step(u, sacc, nacc);
-        if (u + 1 < u1) step(u + 1, nacc, sacc);
+    int u = u0;
+    for (; u + 1 < clear; u += 2) {
+        step(std::false_type{}, u, sacc, nacc);
+        step(std::false_type{}, u + 1, nacc, sacc);
+    }
+    for (; u < u1; u += 2) {
+        step(std::true_type{}, u, sacc, nacc);
+        if (u + 1 < u1) step(std::true_type{}, u + 1, nacc, sacc);
     }
     if (!active) return;
     const float l_tot = l_run + shx(l_run, 32), inv = a.NS > 1 ? 1.f : l_tot == 0.f ? 0.f : 1.f / l_tot;
