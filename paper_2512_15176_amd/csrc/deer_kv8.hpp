@@ -809,8 +809,8 @@ __global__ __launch_bounds__(256, HD == 128 && SRC != KV8_BF16 ? 2 : 3) void k_k
                 }
             }
     };
-    auto softmax = [&](f32x4 (&s)[2][2], bool mask, int page, int hi) {
-        if (mask) {
+    auto softmax = [&](auto masked, f32x4 (&s)[2][2], int page, int hi) {
+        if (decltype(masked)::value) {
 #pragma unroll
             for (int j = 0; j < 2; ++j)
 #pragma unroll
@@ -819,9 +819,11 @@ __global__ __launch_bounds__(256, HD == 128 && SRC != KV8_BF16 ? 2 : 3) void k_k
                     for (int i = 0; i < 4; ++i)
                         if (page * KV8_PAGE + 32 * j + 8 * g + 4 * kb + i >= hi) s[j][kb][i] = -INFINITY;
         }
-        float mx = s[0][0][0];
+        auto at = [&](int e) { return s[e >> 3][(e >> 2) & 1][e & 3]; };
+        float mx = max3(at(0), at(1), at(2)), m1 = max3(at(3), at(4), at(5));
 #pragma unroll
-        for (int e = 1; e < 16; ++e) mx = fmaxf(mx, s[e >> 3][(e >> 2) & 1][e & 3]);
+        for (int e = 6; e < 14; e += 4) { mx = max3(mx, at(e), at(e + 1)); m1 = max3(m1, at(e + 2), at(e + 3)); }
+        mx = fmaxf(max3(mx, at(14), at(15)), m1);
         if (__builtin_amdgcn_ballot_w64((mx - m_run) * a.scale_log2e > KV8_SLACK)) {     // (see kv8_rescale)
             mx = fmaxf(mx, shx(mx, 16));
             const float m_new = fmaxf(m_run, fmaxf(mx, shx(mx, 32)));
@@ -857,24 +859,27 @@ __global__ __launch_bounds__(256, HD == 128 && SRC != KV8_BF16 ? 2 : 3) void k_k
     };
     const int n8 = (sp.max8 + KV8_PAGE - 1) / KV8_PAGE, nh = max(0, sp.hmax - sp.hmin + 1);
     f32x4 s[2][2];
-    for (; u < n8; u += stride) {
-        const bool live = id >= 0;
+    auto page_step = [&](auto masked) {
         const int ask2 = kv8_ask(a.s, table, u + 2 * stride);
         const float ks = ks1, vs = vs1;
         scores(s, [&](int j, int kb, int t) { return dequant8(kc[j][kb][t].x, kc[j][kb][t].y, ks); });
         const int id1 = kv8_page(a.s, ask);
         if (u + stride < n8) load_k(id1);
-        softmax(s, (u + 1) * KV8_PAGE > sp.min8 || !live, u, live ? r.lim8 : 0);
+        softmax(masked, s, u, id >= 0 ? r.lim8 : 0);
         values(s, [&](int j, int c) { return dequant8(vc[j][c].x, vc[j][c].y, vs); });
         if (u + stride < n8) load_v(id1);
         id = id1; ask = ask2;
-    }
+        u += stride;
+    };
+    // (pages that all rows see whole, if they see anything, need no mask: see k_kv8_attn_many)
+    while (u < n8 && (u + 1) * KV8_PAGE <= sp.min8 && id >= 0) page_step(std::false_type{});
+    while (u < n8) page_step(std::true_type{});
     for (; u < n8 + nh; u += stride) {       // hot pages
         const int page = sp.hmin + u - n8;
         const size_t off = (size_t)b * a.hot.seq_stride + (size_t)kvh * a.hot.head_stride + (size_t)((page * KV8_PAGE + a.s.hotbase[b]) & a.hot.mask) * HD;
         const uint4 *kp = (const uint4 *)(a.hot.k + off) + (g & 1) * 32 + krow, *vp = (const uint4 *)(a.hot.v + off) + (g >> 1) * 32 + n;
         scores(s, [&](int j, int kb, int t) { return kp[(j * CB + 2 * t + (g >> 1)) * 64 + 8 * kb]; });
-        softmax(s, true, page, r.h0 < r.lim && r.h0 / KV8_PAGE == page ? r.lim : 0);
+        softmax(std::true_type{}, s, page, r.h0 < r.lim && r.h0 / KV8_PAGE == page ? r.lim : 0);
         values(s, [&](int j, int c) { return vp[(j * CB + (c >> 1) * 2 + (g & 1)) * 64 + (c & 1) * 16]; });
     }
     // the waves' shares meet: every wave adds up a part of the channels

@@ -156,8 +156,9 @@ hipError_t kv8_append(Kv8Cache &c, hipStream_t s, int layer, const T *k, const T
 // 16, 32 rows behind 8000 46 / 40.
 struct Kv8Shares { long long items; int NS; };
 inline Kv8Shares kv8_shares(long long items, long long tiles, int pages) {
-    // key ranges: as many as fill the chip (two workgroups of four waves per compute unit), each with eight pages or its waves' four
-    return Kv8Shares{items, (int)std::max<long long>(1, std::min<long long>({KV8_WGS / std::max<long long>(items, 1), KV8_PART_TILES / std::max<long long>(tiles, 1), 64, (pages + 7) / 8}))};
+    // key ranges: as many as fill the chip (two workgroups of four waves per compute unit), each with eight pages or its waves' four; no more
+    // than 32, which the last workgroup adds up (1 sequence of 32768 tokens in 16, 32 and 64 ranges 25.5, 24.7 and 32.9)
+    return Kv8Shares{items, (int)std::max<long long>(1, std::min<long long>({KV8_WGS / std::max<long long>(items, 1), KV8_PART_TILES / std::max<long long>(tiles, 1), 32, (pages + 7) / 8}))};
 }
 inline double kv8_few_us(const Kv8Shares &s, int pages, int hd) { return 6.0 + 0.008 * (double)s.items * s.NS + 0.0012 * (double)s.items * pages * hd / 128; }
 inline double kv8_many_us(const Kv8Shares &s, int pages, int hd) { return 12.0 + 0.005 * (double)s.items * pages * hd / 128 + (s.NS > 1 ? 5.0 + 0.2 * s.NS : 0.0); }
