@@ -148,23 +148,9 @@ hipError_t kv8_append(Kv8Cache &c, hipStream_t s, int layer, const T *k, const T
            : c.p.head_dim == 64 ? kv8_append_hd<64>(c, s, layer, k, v, k_stride, v_stride) : kv8_append_hd<32>(c, s, layer, k, v, k_stride, v_stride);
 }
 
-// What an attention launch takes, in microseconds, by what it streams: tiles x pages, of 16 packed rows (k_kv8_attn_few) or of 4 x 32
-// (k_kv8_attn_many, with its merge).  Fitted to the heads of the 4B / 8B models and the drafter, 1 to 16 sequences, 1 to 128 rows;
-// good to about 25 %.  few / many measured, heads 32 / 8 of 128: 1 sequence, 32 rows behind 500, 4095, 16000 and 30000 tokens 9.3 / 18.5,
-// 16.2 / 20.8, 30 / 40, 48 / 49; 4 behind 8000 48 / 39; 16 behind 1000 29 / 32, behind 16000 326 / 196; 16 behind 16000 with 8 and
-// 12 rows 128 / 139 and 201 / 165; 8 prompts of 100 20.6 / 11.7.  Heads 14 / 2 of 64: 7 sequences, 31 rows behind 3000 15.8 / 21.8;
-// 16, 32 rows behind 8000 46 / 40.
-struct Kv8Shares { long long items; int NS; };
-inline Kv8Shares kv8_shares(long long items, long long tiles, int pages) {
-    // key ranges: as many as fill the chip (two workgroups of four waves per compute unit), each with eight pages or its waves' four; no more
-    // than 32, which the last workgroup adds up (1 sequence of 32768 tokens in 16, 32 and 64 ranges 25.5, 24.7 and 32.9)
-    return Kv8Shares{items, (int)std::max<long long>(1, std::min<long long>({KV8_WGS / std::max<long long>(items, 1), KV8_PART_TILES / std::max<long long>(tiles, 1), 32, (pages + 7) / 8}))};
-}
-inline double kv8_few_us(const Kv8Shares &s, int pages, int hd) { return 6.0 + 0.008 * (double)s.items * s.NS + 0.0012 * (double)s.items * pages * hd / 128; }
-inline double kv8_many_us(const Kv8Shares &s, int pages, int hd) { return 12.0 + 0.005 * (double)s.items * pages * hd / 128 + (s.NS > 1 ? 5.0 + 0.2 * s.NS : 0.0); }
 // A pool beyond the memory-side cache (256 MB) is streamed past the L2 where a page has one reader: 16 x 32768 tokens of 8 heads
 // of 128 206 -> 186 us, but 16 x 4096, which that cache holds from pass to pass of one layer, 31 -> 34.
-constexpr double KV8_STREAM_BYTES = 256e6;
+constexpr double KV8_SIDE_CACHE = 256e6;
 
 template <typename T>
 hipError_t kv8_read(const Kv8Cache &c, hipStream_t s, int layer, const int *seq, const int *pos, int n, T *k, T *v) {
@@ -174,6 +160,21 @@ hipError_t kv8_read(const Kv8Cache &c, hipStream_t s, int layer, const int *seq,
     return hipGetLastError();
 }
 
+// What an attention launch takes, in microseconds, by what it streams: tiles x pages, of 16 packed rows (k_kv8_attn_few, each of whose
+// tiles reads the pages: from L2 and the memory-side cache, or, where that does not hold them, at a bit more than memory's rate) or of
+// 4 x 32 (k_kv8_attn_many, with its merge).  Fitted to the heads of the 4B / 8B models and the drafter, 1 to 16 sequences, 1 to 128
+// rows; good to about 25 %.  few / many measured, heads 32 / 8 of 128: 1 sequence, 32 rows behind 4095, 16000 and 30000 tokens 16 / 21,
+// 30 / 31, 47 / 41; 4 behind 3000 and 8000 24 / 28, 49 / 37; 16 behind 1000 29 / 31, behind 16000 324 / 177, with 4, 8 and 12 rows there
+// 105 / 124, 127 / 125 and 199 / 146; prompts, 8 of 100 21 / 12, 1 of 500 16 / 18.  Heads 14 / 2 of 64: 7 sequences, 31 rows behind
+// 3000 16 / 21; 16, 32 rows behind 2000 and 8000 16 / 21, 47 / 35.
+struct Kv8Shares { long long items; int NS; };
+inline Kv8Shares kv8_shares(long long items, long long tiles, int pages) {
+    // key ranges: as many as fill the chip (two workgroups of four waves per compute unit), each with eight pages or its waves' four; no more
+    // than 32, which the last workgroup adds up (1 sequence of 32768 tokens in 16, 32 and 64 ranges 25.5, 24.7 and 32.9)
+    return Kv8Shares{items, (int)std::max<long long>(1, std::min<long long>({KV8_WGS / std::max<long long>(items, 1), KV8_PART_TILES / std::max<long long>(tiles, 1), 32, (pages + 7) / 8}))};
+}
+inline double kv8_few_us(const Kv8Shares &s, int pages, int hd, bool big) { return 6.0 + 0.008 * (double)s.items * s.NS + (big ? 0.0021 : 0.0012) * (double)s.items * pages * hd / 128; }
+inline double kv8_many_us(const Kv8Shares &s, int pages, int hd) { return 12.0 + 0.0045 * (double)s.items * pages * hd / 128 + (s.NS > 1 ? 5.0 + 0.2 * s.NS : 0.0); }
 template <int HD, int SRC>
 hipError_t kv8_attend_src(Kv8Cache &c, hipStream_t s, Kv8Attn &a) {
     const int B = c.batch, packed = c.max_new * a.G, pages = (c.max_len + KV8_PAGE - 1) / KV8_PAGE;
@@ -181,10 +182,10 @@ hipError_t kv8_attend_src(Kv8Cache &c, hipStream_t s, Kv8Attn &a) {
     const long long heads = (long long)B * a.Hkv;
     const Kv8Shares f = kv8_shares(heads * rt16, heads * rt16, pages);
     Kv8Shares m = kv8_shares(heads * groups, heads * rt32, pages * 2);      // (a workgroup of this kernel takes four pages at least)
-    if (kv8_few_us(f, pages, HD) <= kv8_many_us(m, pages, HD) && rt16 <= 65535) {
+    if (kv8_few_us(f, pages, HD, (double)heads * pages * (2 * KV8_PAGE * HD) > KV8_SIDE_CACHE) <= kv8_many_us(m, pages, HD) && rt16 <= 65535) {
         a.rts = rt16; a.NS = f.NS;
         const dim3 grid(a.Hkv * a.NS, rt16, B);
-        if (rt16 == 1 && (double)c.p.n_layers * B * pages * c.page_bytes() > KV8_STREAM_BYTES) hipLaunchKernelGGL((k_kv8_attn_few<HD, SRC, true>), grid, dim3(256), 0, s, a);
+        if (rt16 == 1 && (double)c.p.n_layers * B * pages * c.page_bytes() > KV8_SIDE_CACHE) hipLaunchKernelGGL((k_kv8_attn_few<HD, SRC, true>), grid, dim3(256), 0, s, a);
         else hipLaunchKernelGGL((k_kv8_attn_few<HD, SRC, false>), grid, dim3(256), 0, s, a);
         return hipGetLastError();
     }
