@@ -738,7 +738,9 @@ int launch_attn_kv8(deer_ctx *c, int layer, double kv_bytes, const PassRows &row
     Kv8Attn a{};
     a.qhi = w.q_hi; a.qlo = w.q_lo; a.xhi = w.xb_hi; a.xlo = w.xb_lo;
     a.q_row0 = rows.kind == ROWS_PREFILL ? c->kv8.ask_row0 : nullptr;
-    HIPCHK(c, kv8_attend<KV8_FRAG>(c->kv8, c->stream, layer, a, 1.0 / std::sqrt((double)c->m[DEER_TARGET].c.head_dim)));
+    const deer_model_cfg &mc = c->m[DEER_TARGET].c;
+    const double scale = 1.0 / std::sqrt((double)mc.head_dim);
+    HIPCHK(c, mc.n_experts ? kv8_attend<KV8_FRAG2>(c->kv8, c->stream, layer, a, scale) : kv8_attend<KV8_FRAG>(c->kv8, c->stream, layer, a, scale));
     return DEER_OK;
 }
 // A pass's rows go to the hot pages.
@@ -879,7 +881,7 @@ int run_pass(deer_ctx *c, int model, int ntiles, int n_attn, int max_limit, cons
         if (kv_only(l)) { a.Hq = 0; a.kv_fetch_bytes = 0; }
         int rc = launch_gemm<EPI_QKV>(c, a, d, ntiles, 0);
         if (rc) return rc;
-        if (kv8) {
+        if (kv8 && rows_desc.pages_fill) {
             prof_close(c);
             HIPCHK(c, kv8_settle(c->kv8, c->stream, l));
         }
@@ -1040,6 +1042,7 @@ int enqueue_prefill(deer_ctx *c, int batch, const int *ids, const int *lens, con
                 // (sequences without rows in this pass may hold more tokens than those with some)
                 HIPCHK(c, kv8_reserve(k, c->stream, k.ask_start, 0, k.ask_count, 0, batch, pa.n_rows, pa.max_new, k.p.max_seq));
                 k.max_len = pa.maxlim;
+                pr.pages_fill = 1;
                 kv8_place(c, pr);
             }
             if (int rc = run_pass(c, model, (pa.n_rows + 31) / 32, pr.n_desc, pa.maxlim, lm, 0.0, pr)) return rc;
@@ -1384,6 +1387,7 @@ int deer_verify_block(deer_ctx *c, int32_t k, float T, const int32_t *draft_dev)
     double keys = 0;
     for (int b = 0; b < B; ++b) keys += c->h_len[b] - 1 + nrows;
     if (c->kv8_on) {
+        for (int b = 0; b < B; ++b) pr.pages_fill = pr.pages_fill || (c->h_len[b] - 1 + nrows) / KV8_PAGE > (c->h_len[b] - 1) / KV8_PAGE;
         HIPCHK(c, kv8_reserve(c->kv8, c->stream, w.st.len, -1, nullptr, nrows, B, B * nrows, nrows, maxlim));
         kv8_place(c, pr);
     }

@@ -347,6 +347,7 @@ struct PassRows {
     int mask_id, n_fixed;
     int B, share, n_ingest;          // sequences; draft: committed tokens in all that the drafter has not cached
     const int4 *desc; const int *ids; int n_desc;   // prefill
+    int pages_fill;                                 // host: rows may complete pages of an 8-bit cache, or are a long pass's
     const int *slot_base; int slot_mask;            // where a row's K and V go: (slot + slot_base[sequence]) & slot_mask; null: its slot
 };
 struct RowDesc { int tok, pos, slot, seq, qrow; };

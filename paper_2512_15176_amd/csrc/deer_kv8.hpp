@@ -486,9 +486,12 @@ __global__ __launch_bounds__(256) void k_kv8_read(Kv8State s, const int *__restr
 //   of a group of four fills four of a tile's 32 operand rows and a block of 32 fills four tiles.  S^T = K Q^T and O^T = V^T P^T as
 //   in k_attn; e4m3 becomes bf16 (exactly, with the page's scale) on its way to the matrix instruction.
 //   Q and P enter as NQ and NP bf16 planes: one where q and the result are bf16 (q is exact; P is rounded by at most 2^-9 of itself,
-//   less than the result's own rounding), three for float32 (24 bits), two for the engine's fragments (its Q has two planes).
+//   less than the result's own rounding), three for float32 (24 bits).  The engine's fragments: one for a dense model, as the low
+//   plane of its Q would add nine bits to scores whose keys have four (verify pass of 12 layers of the 8B model, 16 x 32768 tokens:
+//   12.2 ms with both planes, 10.3 with one); two for a mixture, whose rows that lie between two experts go to the other one after
+//   any rounding (one plane: a row of the tests did, and its logits were 0.1 off).
 // ------------------------------------------------------------------------------------------
-enum { KV8_BF16 = 0, KV8_F32 = 1, KV8_FRAG = 2 };   // where q comes from and the result goes: rows, or the engine's fragments
+enum { KV8_BF16 = 0, KV8_F32 = 1, KV8_FRAG = 2, KV8_FRAG2 = 3 };   // where q comes from and the result goes: rows, or the engine's fragments
 
 struct Kv8Attn {
     Kv8State s;
@@ -548,7 +551,7 @@ __device__ __forceinline__ Kv8Row kv8_row(const Kv8Attn &a, int b, int kvh, int 
 }
 
 template <int HD, int SRC>
-struct Kv8Planes { static constexpr int N = SRC == KV8_BF16 ? 1 : SRC == KV8_F32 ? 3 : 2; };
+struct Kv8Planes { static constexpr int N = SRC == KV8_F32 ? 3 : SRC == KV8_FRAG2 ? 2 : 1; };
 
 // q elements e0 .. e0 + 7 of a lane's row, as planes
 template <int HD, int SRC>
@@ -568,7 +571,7 @@ __device__ __forceinline__ void kv8_q8(const Kv8Attn &a, const Kv8Row &r, int b,
         const int ar = r.row < 0 ? 0 : (a.q_row0 ? a.q_row0[b] : 32 * b) + r.row - a.s.cu[b];
         const size_t vec = ((size_t)((ar >> 5) * a.Hq + r.head) * (HD / 16)) * 64 + frag_vec(ar & 31, e0 >> 3);
         o[0] = r.row < 0 ? zero : a.qhi[vec];
-        o[1] = r.row < 0 ? zero : a.qlo[vec];
+        if constexpr (SRC == KV8_FRAG2) o[1] = r.row < 0 ? zero : a.qlo[vec];
     }
 }
 // Q fragments of a tile: [plane][k-step]
@@ -628,7 +631,7 @@ __device__ __forceinline__ void kv8_store(const Kv8Attn &a, const Kv8Row &r, int
         const int q = 2 * hh + i;
         // (a row that sees nothing is not masked where the others of its tile need no mask)
         const float v0 = r.lim > 0 ? o[4 * i] : 0.f, v1 = r.lim > 0 ? o[4 * i + 1] : 0.f, v2 = r.lim > 0 ? o[4 * i + 2] : 0.f, v3 = r.lim > 0 ? o[4 * i + 3] : 0.f;
-        if constexpr (SRC == KV8_FRAG) {    // the partner lane holds the other half of an octet: see attn_write_frag
+        if constexpr (SRC >= KV8_FRAG) {    // the partner lane holds the other half of an octet: see attn_write_frag
             const float w0 = shx(v0, 32), w1 = shx(v1, 32), w2 = shx(v2, 32), w3 = shx(v3, 32);
             if (i == half && r.row >= 0) {
                 const float v[8] = {half ? w0 : v0, half ? w1 : v1, half ? w2 : v2, half ? w3 : v3, half ? v0 : w0, half ? v1 : w1, half ? v2 : w2, half ? v3 : w3};
@@ -735,7 +738,7 @@ template <int HD>
 struct Kv8Part16 { static constexpr int FLOATS = 16 * HD + 32; };   // per (tile of 16, kv head, range): O [HD/16][64 lanes][4], (M, L)[16]
 
 template <int HD, int SRC, bool STREAM>
-__global__ __launch_bounds__(256, HD == 128 && SRC != KV8_BF16 ? 2 : 3) void k_kv8_attn_few(const Kv8Attn a) {
+__global__ __launch_bounds__(256, HD == 128 && (SRC == KV8_F32 || SRC == KV8_FRAG2) ? 2 : 3) void k_kv8_attn_few(const Kv8Attn a) {
     constexpr int T = HD / 32, CB = HD / 16, N = Kv8Planes<HD, SRC>::N, PF = Kv8Part16<HD>::FLOATS;   // T: k-steps of 32, and chunks per 32 keys
     constexpr int W = 4, NB = (CB + W - 1) / W;        // waves; channel blocks that a wave adds up
     __shared__ float4 s_o[4][CB][64];
@@ -961,7 +964,7 @@ __global__ __launch_bounds__(256, HD == 128 && SRC != KV8_BF16 ? 2 : 3) void k_k
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[k][e] = r.lim > 0 ? o[k][e] * inv : 0.f;
         const int ch = (w + k * W) * 16 + 4 * g;
-        if constexpr (SRC == KV8_FRAG) {     // lanes 16 apart hold the two halves of an octet: one writes its high plane, one its low
+        if constexpr (SRC >= KV8_FRAG) {     // lanes 16 apart hold the two halves of an octet: one writes its high plane, one its low
             const float x0 = shx(o[k][0], 16), x1 = shx(o[k][1], 16), x2 = shx(o[k][2], 16), x3 = shx(o[k][3], 16);
             const bool odd = g & 1;
             const float v8[8] = {odd ? x0 : o[k][0], odd ? x1 : o[k][1], odd ? x2 : o[k][2], odd ? x3 : o[k][3], odd ? o[k][0] : x0, odd ? o[k][1] : x1, odd ? o[k][2] : x2, odd ? o[k][3] : x3};

@@ -187,7 +187,14 @@ assert lib.deer_draft_block(ctx, 5, C.c_float(0.0), 0, draft) == 0
 launches()
 assert lib.deer_verify_block(ctx, 5, C.c_float(0.0), draft) == 0
 names = [n for n, g in launches()]
-assert count("k_kv8_reserve") == 1 and count("k_kv8_settle") == 5 and count("k_kv8_attn") == 5
+assert count("k_kv8_reserve") == 1 and count("k_kv8_settle") == 5 and count("k_kv8_attn") == 5      # 59 + 5 tokens: a page fills
+assert lib.deer_debug_force_commit(ctx, (C.c_int32 * 2)(1, 1), (C.c_int32 * 2)(1, 1), 1) == 0
+assert pre([130, 40]) == 0
+assert lib.deer_draft_block(ctx, 5, C.c_float(0.0), 0, draft) == 0
+launches()
+assert lib.deer_verify_block(ctx, 5, C.c_float(0.0), draft) == 0
+names = [n for n, g in launches()]
+assert count("k_kv8_settle") == 0 and count("k_kv8_attn") == 5          # none does
 assert not any("k_attn" in n for n in names)
 print("done")
 """)
