@@ -238,7 +238,8 @@ int deer_kv8_init(const deer_kv8_params *p, void *cache_dev, void *workspace_dev
 
 /* The tables of a pass.  Sequence b < batch keeps its first start_dev[b] tokens (0: none; fewer than it holds: the others are
  * dropped) and takes new_dev[b] rows at positions start_dev[b] ..; it then holds the pages of start + new tokens, others go back to
- * the pool.  The rows of the pass are those of sequence 0, then 1, ..  Other sequences keep what they hold.
+ * the pool.  The rows of the pass are those of sequence 0, then 1, ..  Other sequences keep what they hold.  start_dev may be the
+ * handle's own lengths (deer_kv8_get_tables): rows behind what every sequence holds, also where the call is captured and replayed.
  * Host bounds, for launch shapes: rows >= the sum of new_dev, max_new >= its largest, max_len >= the largest start + new.
  * Refused, one by one and on the device (deer_kv8_status): a sequence with numbers outside these bounds, with start beyond its
  * tokens, or with a start inside a page whose bf16 rows are gone; and, in order of sequence, the first that the free pages do not
@@ -251,12 +252,15 @@ int deer_kv8_reserve(deer_kv8 *c, int32_t batch, const int32_t *start_dev, const
 
 /* The pass's rows of one layer, [rows][n_kv_heads][head_dim], enter the cache: F32 (rounded to bf16, nearest even) or BF16; strides
  * between rows in elements (a slice of a fused projection is fine), addresses and strides multiples of 16 bytes.  Pages that the
- * rows complete are quantised.  A row with an infinity or NaN in a head makes every row that sees it NaN there, and no other. */
+ * rows complete are quantised.  Once per layer and pass; a pass with max_new above 64 serves one layer after the other: each layer's
+ * deer_kv8_attend before the next layer's append (else DEER_ESTATE).  A row with an infinity or NaN in a head makes every row that
+ * sees it NaN there, and no other. */
 int deer_kv8_append(deer_kv8 *c, int32_t layer, const void *k_dev, const void *v_dev, int dtype, int64_t k_stride, int64_t v_stride, int32_t rows);
 
 /* Attention of the pass's rows q [rows][n_q_heads][head_dim] over one layer, behind its deer_kv8_append: out = softmax(scale q K^T) V,
  * query head h with kv head h / (n_q_heads / n_kv_heads).  limits_dev[row]: how many of its sequence's keys a row sees, from the first
- * (cut to 0 .. the tokens held; 0: the result is zeros); NULL: its position + 1 (causal).  scale 0: 1 / sqrt(head_dim).  dtype is that
+ * (cut to 0 .. the tokens held; 0: the result is zeros; what ends before the pass's first page is read in 8 bits throughout); NULL:
+ * its position + 1 (causal).  scale 0: 1 / sqrt(head_dim).  dtype is that
  * of q and out, F32 (computed to about 2^-22) or BF16; softmax and sums are in fp32.  Rows may be read as often as wanted. */
 int deer_kv8_attend(deer_kv8 *c, int32_t layer, const void *q_dev, int dtype, int64_t q_stride, const int32_t *limits_dev, float scale, void *out_dev,
                     int64_t out_stride, int32_t rows);

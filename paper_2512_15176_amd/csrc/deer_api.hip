@@ -1777,6 +1777,7 @@ int deer_kv8_append(deer_kv8 *c, int32_t layer, const void *k_dev, const void *v
     if (c->c.batch == 0) return fail8(c, DEER_ESTATE, "append needs the tables of a pass (deer_kv8_reserve)");
     if (layer < 0 || layer >= p.n_layers) return fail8(c, DEER_EINVAL, "layer out of range");
     if (rows != c->c.rows) return fail8(c, DEER_EINVAL, "rows must be those of the pass");
+    if (c->c.long_pass && layer == c->c.scratch_layer) return fail8(c, DEER_ESTATE, "the rows of a long pass enter a layer once");
     if (rows == 0) return DEER_OK;
     const int64_t width = (int64_t)p.n_kv_heads * p.head_dim;
     if (!k_dev || !v_dev || !aligned16(k_dev) || !aligned16(v_dev)) return fail8(c, DEER_EINVAL, "null or unaligned pointer");
@@ -1796,6 +1797,7 @@ int deer_kv8_attend(deer_kv8 *c, int32_t layer, const void *q_dev, int dtype, in
     if (c->c.batch == 0) return fail8(c, DEER_ESTATE, "attend needs the tables of a pass (deer_kv8_reserve)");
     if (layer < 0 || layer >= p.n_layers) return fail8(c, DEER_EINVAL, "layer out of range");
     if (rows != c->c.rows) return fail8(c, DEER_EINVAL, "rows must be those of the pass");
+    if (c->c.long_pass && layer != c->c.scratch_layer) return fail8(c, DEER_ESTATE, "a layer's attention over a long pass must follow its append, before another layer's");
     if (!(scale >= 0.f && scale < 1e30f)) return fail8(c, DEER_EINVAL, "scale must be positive, or 0 for 1 / sqrt(head_dim)");
     if (rows == 0) return DEER_OK;
     const int64_t width = (int64_t)p.n_q_heads * p.head_dim;

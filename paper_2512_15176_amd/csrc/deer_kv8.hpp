@@ -91,9 +91,9 @@ __global__ void k_kv8_init(Kv8State s) {
 // A sequence is refused (keeps its pages and tokens, gets no rows) for numbers out of range, a start behind its tokens, a start
 // inside a page whose bf16 rows are gone, or, like every growing one behind it, where the pages do not suffice.
 // Every workgroup works out all sequences (one scan) and writes its share of table entries and rows, four rows to a thread; the
-// state itself is written by the last to arrive, when all have read it.  Bound by latency: 16 sequences 4 us, 1000 prompts with
-// 512500 rows 9 us (their 6.1 MB would take 1).  grid: any; 1024 threads; B <= 1024.
-__global__ __launch_bounds__(1024) void k_kv8_reserve(Kv8State s, const int *__restrict__ start, int start_add, const int *__restrict__ count,
+// state itself is written by the last to arrive, when all have read it (so that start may be the lengths themselves).  Bound by latency:
+// 16 sequences 4 to 6 us, 1000 prompts with 512500 rows 13 us (their 6.1 MB would take 1).  grid: any; 1024 threads; B <= 1024.
+__global__ __launch_bounds__(1024) void k_kv8_reserve(Kv8State s, const int *start, int start_add, const int *__restrict__ count,
                                                       int count_const, int B, int rows, int max_new, int max_len, int scratch) {
     __shared__ int s_row[KV8_MAX_BATCH], s_start[KV8_MAX_BATCH], s_n[KV8_MAX_BATCH], s_held[KV8_MAX_BATCH], s_tp[KV8_MAX_BATCH],
         s_grow[KV8_MAX_BATCH], s_give[KV8_MAX_BATCH], s_taken, s_given, s_refused, s_flag;
@@ -503,7 +503,7 @@ struct Kv8Attn {
     const uint4 *qhi, *qlo; uint4 *xhi, *xlo;      // fragments
     const int *q_row0;                             // fragments: attention row of a sequence's first row; null: 32 * sequence
     float *part; int *counters;                    // counters: zero between kernels
-    int Hq, Hkv, G, rows, NS, rts;                 // NS key ranges; rts: tiles of 32 packed rows per sequence
+    int Hq, Hkv, G, NS, rts;                       // NS key ranges; rts: tiles of packed rows per sequence
     float scale_log2e, m_init;
 };
 
@@ -1153,7 +1153,7 @@ __global__ __launch_bounds__(256, HD == 128 && SRC == KV8_F32 ? 1 : 2) void k_kv
     }
     if (!active) return;
     const float l_tot = l_run + shx(l_run, 32), inv = a.NS > 1 ? 1.f : l_tot == 0.f ? 0.f : 1.f / l_tot;
-    float *pp = a.part + ((size_t)((b * a.rts + rt) * a.Hkv + kvh) * a.NS + split) * AttnPartial<HD>::FLOATS;
+    float *pp = a.part + (((size_t)(b * a.rts + rt) * a.Hkv + kvh) * a.NS + split) * AttnPartial<HD>::FLOATS;
     if (a.NS > 1 && lane < 32) *(float2 *)(pp + 32 * HD + 2 * lane) = make_float2(m_run, l_tot);
 #pragma unroll
     for (int tt = 0; tt < HT; ++tt)

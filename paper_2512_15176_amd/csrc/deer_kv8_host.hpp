@@ -25,7 +25,8 @@ struct Kv8Cache {
     size_t scratch_slots = 0, cache_bytes = 0, work_bytes = 0;
     // the pass
     int batch = 0, rows = 0, max_new = 0, max_len = 0;
-    bool long_pass = false;      // rows in the scratch
+    bool long_pass = false;      // rows in the scratch ..
+    int scratch_layer = -1;      // .. of this layer
 
     size_t page_bytes() const { return (size_t)p.n_kv_heads * 2 * KV8_PAGE * p.head_dim; }
     size_t ring_layer() const { return (size_t)p.max_batch * p.n_kv_heads * KV8_SLOTS * p.head_dim; }   // elements of K, and of V
@@ -108,6 +109,7 @@ inline hipError_t kv8_reserve(Kv8Cache &c, hipStream_t s, const int *start, int 
     max_new = std::min(max_new, std::max(rows, 0));
     c.batch = batch; c.rows = rows; c.max_new = max_new; c.max_len = max_len;
     c.long_pass = max_new > KV8_PAGE;
+    c.scratch_layer = -1;
     // four rows to a thread; a call without rows only gives pages back, up to the batch's tables
     const long long work = rows ? rows : std::min<long long>(c.p.n_pages, (long long)batch * c.st.max_blocks);
     const int wgs = (int)std::max<long long>(1, std::min<long long>(256, (work + 4095) / 4096));
@@ -144,6 +146,7 @@ hipError_t kv8_append_hd(Kv8Cache &c, hipStream_t s, int layer, const T *k, cons
 template <typename T>
 hipError_t kv8_append(Kv8Cache &c, hipStream_t s, int layer, const T *k, const T *v, size_t k_stride, size_t v_stride) {
     if (c.rows == 0 || c.max_new == 0) return hipSuccess;
+    c.scratch_layer = layer;
     return c.p.head_dim == 128 ? kv8_append_hd<128>(c, s, layer, k, v, k_stride, v_stride)
            : c.p.head_dim == 64 ? kv8_append_hd<64>(c, s, layer, k, v, k_stride, v_stride) : kv8_append_hd<32>(c, s, layer, k, v, k_stride, v_stride);
 }
@@ -200,7 +203,7 @@ template <int SRC>
 hipError_t kv8_attend(Kv8Cache &c, hipStream_t s, int layer, Kv8Attn a, double scale) {
     if (c.rows == 0 || c.max_new == 0) return hipSuccess;
     a.s = c.st; a.hot = c.hot_view(layer); a.pages = c.layer_pages(layer); a.scales = c.layer_scales(layer);
-    a.part = c.part; a.counters = c.counters; a.Hq = c.p.n_q_heads; a.Hkv = c.p.n_kv_heads; a.G = a.Hq / a.Hkv; a.rows = c.rows;
+    a.part = c.part; a.counters = c.counters; a.Hq = c.p.n_q_heads; a.Hkv = c.p.n_kv_heads; a.G = a.Hq / a.Hkv;
     a.scale_log2e = (float)(scale * 1.4426950408889634);
     a.m_init = -3e38f / std::max(1.f, a.scale_log2e);     // times scale_log2e it stays finite
     return c.p.head_dim == 128 ? kv8_attend_src<128, SRC>(c, s, a) : c.p.head_dim == 64 ? kv8_attend_src<64, SRC>(c, s, a) : kv8_attend_src<32, SRC>(c, s, a);

@@ -199,3 +199,14 @@ assert not any("k_attn" in n for n in names)
 print("done")
 """)
     assert "done" in out
+
+
+def test_a_long_pass_serves_one_layer_after_the_other(tmp_path):
+    run(tmp_path, """
+A = lambda layer: lib.deer_kv8_append(kv, layer, rows, rows, 1, 128, 128, 200)
+Q = lambda layer: lib.deer_kv8_attend(kv, layer, rows, 1, 512, None, 0.0, rows, 512, 200)
+R = lambda n: lib.deer_kv8_reserve(kv, 4, ints, ints, 200, n, 500)
+assert R(65) == 0 and Q(0) == -2 and A(0) == 0 and Q(0) == 0 and Q(0) == 0 and A(0) == -2 and Q(1) == -2
+assert A(1) == 0 and Q(0) == -2 and Q(1) == 0
+assert R(64) == 0 and A(0) == 0 and A(1) == 0 and Q(0) == 0 and Q(1) == 0 and A(0) == 0
+""")
