@@ -467,3 +467,87 @@ def test_arguments_are_checked():
     p.kv.close()
     with pytest.raises(RuntimeError):
         p.kv.attend(0, x(8, 8, 64))
+
+
+def test_a_captured_loop_over_the_handles_own_lengths():
+    """A prompt and single tokens behind what the sequences hold (start: the cache's lengths), captured and replayed over two layers."""
+    import torch
+    from paper_2512_15176_amd import Kv8Cache
+    hq, hkv, hd, L = 8, 2, 64, 2
+    rng = np.random.default_rng(17)
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        a, b = (Kv8Cache(L, hq, hkv, hd, 3, 1024, max_rows=600) for _ in range(2))
+        zero = torch.zeros(3, dtype=torch.int32, device="cuda")
+        count = {n: torch.tensor([n, 0, n], dtype=torch.int32, device="cuda") for n in (1, 150)}
+        data = {n: [torch.randn(2 * n, h, hd, device="cuda", dtype=torch.bfloat16) for h in (hkv, hkv, hq)] for n in (1, 150)}
+
+        def one(kv, start, n):
+            kv.reserve(start, count[n], 2 * n, n, 1024)
+            outs = []
+            for layer in range(L):
+                kv.append(layer, data[n][0] * (layer + 1), data[n][1])
+                outs.append(kv.attend(layer, data[n][2]))
+            return torch.stack(outs)
+
+        for n in (1, 150):
+            one(a, a.lengths, n)
+        side.synchronize()
+        graphs = {}
+        for n in (1, 150):
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g, stream=side):
+                out = one(a, a.lengths, n)
+            graphs[n] = (g, out)
+        a.reserve(zero, zero, 0, 0, 0)
+        held = [0, 0, 0]
+        for n in (150, 1, 1, 150, 1, 150, 1, 1):
+            for t in data[n]:
+                t.copy_(torch.from_numpy(rng.standard_normal(tuple(t.shape)).astype(np.float32)))
+            graphs[n][0].replay()
+            want = one(b, torch.tensor(held, dtype=torch.int32, device="cuda"), n)
+            held = [held[0] + n, 0, held[2] + n]
+            assert torch.equal(graphs[n][1], want) and a.lengths.tolist() == held == b.lengths.tolist()
+            taken = a.block_table[a.block_table >= 0].tolist()        # (not b's pages: those that a's first passes gave back lie in another order)
+            assert len(taken) == len(set(taken)) == int(a.pages_held.sum()) == sum(-(-x // 64) for x in held)
+    a.close()
+    b.close()
+
+
+def test_two_caches_work_at_once():
+    """Two handles on two streams, whose passes overlap, give what each gives alone."""
+    import torch
+    from paper_2512_15176_amd import Kv8Cache
+    hq, hkv, hd = 8, 2, 128
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    g = torch.Generator(device="cuda").manual_seed(1)
+    k, v, q = (torch.randn(2, 2000, h, hd, generator=g, device="cuda", dtype=torch.bfloat16) for h in (hkv, hkv, hq))
+    n = torch.tensor([2000], dtype=torch.int32, device="cuda")
+    zero, one = torch.zeros_like(n), torch.ones_like(n)
+    torch.cuda.synchronize()
+    outs = {}
+    for alone in (True, False):
+        caches = []
+        for s in streams:
+            with torch.cuda.stream(s):
+                caches.append(Kv8Cache(1, hq, hkv, hd, 1, 4096, max_rows=2000))
+        got = [[], []]
+        for i in range(6):
+            for j, s in enumerate(streams):
+                with torch.cuda.stream(s):
+                    if i == 0:
+                        caches[j].reserve(zero, n, 2000, 2000, 2000)
+                        caches[j].append(0, k[j], v[j])
+                        got[j].append(caches[j].attend(0, q[j]))
+                    else:
+                        caches[j].reserve(caches[j].lengths, one, 1, 1, 4096)
+                        caches[j].append(0, k[j, i:i + 1], v[j, i:i + 1])
+                        got[j].append(caches[j].attend(0, q[j, i:i + 1]))
+                if alone:
+                    torch.cuda.synchronize()
+        torch.cuda.synchronize()
+        outs[alone] = [torch.cat(x) for x in got]
+        for kv in caches:
+            kv.close()
+    for j in range(2):
+        assert torch.equal(outs[True][j], outs[False][j])
