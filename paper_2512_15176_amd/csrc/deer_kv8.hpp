@@ -737,8 +737,12 @@ __device__ __forceinline__ uint2 load8_stream(const uint8_t *p) {
 template <int HD>
 struct Kv8Part16 { static constexpr int FLOATS = 16 * HD + 32; };   // per (tile of 16, kv head, range): O [HD/16][64 lanes][4], (M, L)[16]
 
+// its workgroups that a compute unit holds
+template <int HD, int SRC>
+constexpr int kv8_few_resident() { return HD == 128 && (SRC == KV8_F32 || SRC == KV8_FRAG2) ? 2 : 3; }
+
 template <int HD, int SRC, bool STREAM>
-__global__ __launch_bounds__(256, HD == 128 && (SRC == KV8_F32 || SRC == KV8_FRAG2) ? 2 : 3) void k_kv8_attn_few(const Kv8Attn a) {
+__global__ __launch_bounds__(256, (kv8_few_resident<HD, SRC>())) void k_kv8_attn_few(const Kv8Attn a) {
     constexpr int T = HD / 32, CB = HD / 16, N = Kv8Planes<HD, SRC>::N, PF = Kv8Part16<HD>::FLOATS;   // T: k-steps of 32, and chunks per 32 keys
     constexpr int W = 4, NB = (CB + W - 1) / W;        // waves; channel blocks that a wave adds up
     __shared__ float4 s_o[4][CB][64];

@@ -171,10 +171,14 @@ hipError_t kv8_read(const Kv8Cache &c, hipStream_t s, int layer, const int *seq,
 // 105 / 124, 127 / 125 and 199 / 146; prompts, 8 of 100 21 / 12, 1 of 500 16 / 18.  Heads 14 / 2 of 64: 7 sequences, 31 rows behind
 // 3000 16 / 21; 16, 32 rows behind 2000 and 8000 16 / 21, 47 / 35.
 struct Kv8Shares { long long items; int NS; };
-inline Kv8Shares kv8_shares(long long items, long long tiles, int pages) {
+inline Kv8Shares kv8_shares(long long items, long long tiles, int pages, int resident) {
     // key ranges: as many as fill the chip (two workgroups of four waves per compute unit), each with eight pages or its waves' four; no more
-    // than 32, which the last workgroup adds up (1 sequence of 32768 tokens in 16, 32 and 64 ranges 25.5, 24.7 and 32.9)
-    return Kv8Shares{items, (int)std::max<long long>(1, std::min<long long>({KV8_WGS / std::max<long long>(items, 1), KV8_PART_TILES / std::max<long long>(tiles, 1), 32, (pages + 7) / 8}))};
+    // than 32, which the last workgroup adds up (1 sequence of 32768 tokens in 16, 32 and 64 ranges 25.5, 24.7 and 32.9).  257 to 384 items
+    // take two where a compute unit holds three workgroups (bf16, heads 32 / 4 of 128, 8 x 17 rows behind 300 .. 3000 tokens 25.1 -> 20.7;
+    // 32 / 8, 14 x 12 behind 8000 83 -> 65; float32 heads 14 / 2 of 64, 16 x 21 behind 8000 61 -> 46), but not where it holds two (float32
+    // 32 / 4 of 128, 9 x 17 behind 400 .. 3000 28.5 -> 29.4)
+    const long long fill = std::max<long long>(KV8_WGS / std::max<long long>(items, 1), resident > 2 && items * 2 <= KV8_WGS / 2 * resident ? 2 : 1);
+    return Kv8Shares{items, (int)std::max<long long>(1, std::min<long long>({fill, KV8_PART_TILES / std::max<long long>(tiles, 1), 32, (pages + 7) / 8}))};
 }
 inline double kv8_few_us(const Kv8Shares &s, int pages, int hd, bool big) { return 6.0 + 0.008 * (double)s.items * s.NS + (big ? 0.0021 : 0.0012) * (double)s.items * pages * hd / 128; }
 inline double kv8_many_us(const Kv8Shares &s, int pages, int hd) { return 12.0 + 0.0045 * (double)s.items * pages * hd / 128 + (s.NS > 1 ? 5.0 + 0.2 * s.NS : 0.0); }
@@ -183,8 +187,8 @@ hipError_t kv8_attend_src(Kv8Cache &c, hipStream_t s, Kv8Attn &a) {
     const int B = c.batch, packed = c.max_new * a.G, pages = (c.max_len + KV8_PAGE - 1) / KV8_PAGE;
     const int rt16 = (packed + 15) / 16, rt32 = (packed + 31) / 32, groups = (rt32 + 3) / 4;
     const long long heads = (long long)B * a.Hkv;
-    const Kv8Shares f = kv8_shares(heads * rt16, heads * rt16, pages);
-    Kv8Shares m = kv8_shares(heads * groups, heads * rt32, pages * 2);      // (a workgroup of this kernel takes four pages at least)
+    const Kv8Shares f = kv8_shares(heads * rt16, heads * rt16, pages, kv8_few_resident<HD, SRC>());
+    const Kv8Shares m = kv8_shares(heads * groups, heads * rt32, pages * 2, 2);      // (a workgroup of this kernel takes four pages at least)
     if (kv8_few_us(f, pages, HD, (double)heads * pages * (2 * KV8_PAGE * HD) > KV8_SIDE_CACHE) <= kv8_many_us(m, pages, HD) && rt16 <= 65535) {
         a.rts = rt16; a.NS = f.NS;
         const dim3 grid(a.Hkv * a.NS, rt16, B);
