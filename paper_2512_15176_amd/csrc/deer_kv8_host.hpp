@@ -163,13 +163,15 @@ hipError_t kv8_read(const Kv8Cache &c, hipStream_t s, int layer, const int *seq,
     return hipGetLastError();
 }
 
-// What an attention launch takes, in microseconds, by what it streams: tiles x pages, of 16 packed rows (k_kv8_attn_few, each of whose
-// tiles reads the pages: from L2 and the memory-side cache, or, where that does not hold them, at a bit more than memory's rate) or of
-// 4 x 32 (k_kv8_attn_many, with its merge).  Fitted to the heads of the 4B / 8B models and the drafter, 1 to 16 sequences, 1 to 128
-// rows; good to about 25 %.  few / many measured, heads 32 / 8 of 128: 1 sequence, 32 rows behind 4095, 16000 and 30000 tokens 16 / 21,
-// 30 / 31, 47 / 41; 4 behind 3000 and 8000 24 / 28, 49 / 37; 16 behind 1000 29 / 31, behind 16000 324 / 177, with 4, 8 and 12 rows there
-// 105 / 124, 127 / 125 and 199 / 146; prompts, 8 of 100 21 / 12, 1 of 500 16 / 18.  Heads 14 / 2 of 64: 7 sequences, 31 rows behind
-// 3000 16 / 21; 16, 32 rows behind 2000 and 8000 16 / 21, 47 / 35.
+// What an attention launch takes, in microseconds, by what it streams: k_kv8_attn_few tiles of 16 packed rows x the pages that they see,
+// each read by every tile (from L2 and the memory-side cache); k_kv8_attn_many pages, which a workgroup reads once, and tiles of 32 x
+// pages, by the planes that Q and P enter as, with its merge.  The pages are what a row sees on average: a prompt's rows half of its own.
+// Fitted to 350 calls of bf16 and float32, heads 32 / 8 and 32 / 4 of 128 and 14 / 2 of 64, 1 to 16 sequences of 0 to 16000 tokens, 1 to
+// 2000 rows: the choice costs 0.5 % of the better kernel's time on average and 19 % at most.  few / many measured, bf16: heads 32 / 8, 1
+// sequence, 32 rows behind 8000 and 16000 tokens 20 / 25, 30 / 31, 200 rows behind 8000 82 / 46; 8 sequences, 8, 17 and 32 rows behind
+// 8000 31 / 37, 62 / 45, 83 / 52; 16, 8 and 17 rows behind 16000 127 / 127, 252 / 158; heads 32 / 4, 4 sequences, 17 rows behind
+// 16000 60 / 43; heads 14 / 2, 16 sequences, 17 rows behind 2000 and 16000 14 / 16, 47 / 36; prompts, 1 of 500 16 / 19.  Float32: heads
+// 32 / 8, 8 sequences, 32 rows behind 2000 and 8000 32 / 56, 97 / 107, prompts, 1 of 1000 and 2000 46 / 57, 125 / 110.
 struct Kv8Shares { long long items; int NS; };
 inline Kv8Shares kv8_shares(long long items, long long tiles, int pages, int resident) {
     // key ranges: as many as fill the chip (two workgroups of four waves per compute unit), each with eight pages or its waves' four; no more
@@ -180,8 +182,10 @@ inline Kv8Shares kv8_shares(long long items, long long tiles, int pages, int res
     const long long fill = std::max<long long>(KV8_WGS / std::max<long long>(items, 1), resident > 2 && items * 2 <= KV8_WGS / 2 * resident ? 2 : 1);
     return Kv8Shares{items, (int)std::max<long long>(1, std::min<long long>({fill, KV8_PART_TILES / std::max<long long>(tiles, 1), 32, (pages + 7) / 8}))};
 }
-inline double kv8_few_us(const Kv8Shares &s, int pages, int hd, bool big) { return 6.0 + 0.008 * (double)s.items * s.NS + (big ? 0.0021 : 0.0012) * (double)s.items * pages * hd / 128; }
-inline double kv8_many_us(const Kv8Shares &s, int pages, int hd) { return 12.0 + 0.0045 * (double)s.items * pages * hd / 128 + (s.NS > 1 ? 5.0 + 0.2 * s.NS : 0.0); }
+inline double kv8_few_us(const Kv8Shares &s, double pages, int hd) { return 6.0 + 0.005 * (double)s.items * s.NS + 0.0012 * (double)s.items * pages * hd / 128; }
+inline double kv8_many_us(const Kv8Shares &s, long long heads, int rt32, double pages, int hd, int planes) {
+    return 10.0 + (0.0008 + (0.0002 + 0.0011 * planes) * rt32) * (double)heads * pages * hd / 128 + (s.NS > 1 ? 5.0 + 0.2 * s.NS : 0.0);
+}
 template <int HD, int SRC>
 hipError_t kv8_attend_src(Kv8Cache &c, hipStream_t s, Kv8Attn &a) {
     const int B = c.batch, packed = c.max_new * a.G, pages = (c.max_len + KV8_PAGE - 1) / KV8_PAGE;
@@ -189,7 +193,8 @@ hipError_t kv8_attend_src(Kv8Cache &c, hipStream_t s, Kv8Attn &a) {
     const long long heads = (long long)B * a.Hkv;
     const Kv8Shares f = kv8_shares(heads * rt16, heads * rt16, pages, kv8_few_resident<HD, SRC>());
     const Kv8Shares m = kv8_shares(heads * groups, heads * rt32, pages * 2, 2);      // (a workgroup of this kernel takes four pages at least)
-    if (kv8_few_us(f, pages, HD, (double)heads * pages * (2 * KV8_PAGE * HD) > KV8_SIDE_CACHE) <= kv8_many_us(m, pages, HD) && rt16 <= 65535) {
+    const double seen = (c.max_len - 0.5 * c.max_new) / KV8_PAGE + 0.5;
+    if (kv8_few_us(f, seen, HD) <= kv8_many_us(m, heads, rt32, seen, HD, Kv8Planes<HD, SRC>::N) && rt16 <= 65535) {
         a.rts = rt16; a.NS = f.NS;
         const dim3 grid(a.Hkv * a.NS, rt16, B);
         if (rt16 == 1 && (double)c.p.n_layers * B * pages * c.page_bytes() > KV8_SIDE_CACHE) hipLaunchKernelGGL((k_kv8_attn_few<HD, SRC, true>), grid, dim3(256), 0, s, a);
