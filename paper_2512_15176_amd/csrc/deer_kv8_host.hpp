@@ -164,8 +164,10 @@ hipError_t kv8_read(const Kv8Cache &c, hipStream_t s, int layer, const int *seq,
 }
 
 // What an attention launch takes, in microseconds, by what it streams: k_kv8_attn_few tiles of 16 packed rows x the pages that they see,
-// each read by every tile (from L2 and the memory-side cache); k_kv8_attn_many pages, which a workgroup reads once, and tiles of 32 x
-// pages, by the planes that Q and P enter as, with its merge.  The pages are what a row sees on average: a prompt's rows half of its own.
+// each read by every tile (from L2 and the memory-side cache; fewer workgroups than fill the chip take no less time: 3 sequences, 32
+// rows behind 8000 tokens of heads 32 / 8, 384 workgroups 47, k_kv8_attn_many 34); k_kv8_attn_many pages, which a workgroup reads once,
+// and tiles of 32 x pages, by the planes that Q and P enter as, with its merge.  The pages are what a row sees on average: a prompt's
+// rows half of its own.
 // Fitted to 350 calls of bf16 and float32, heads 32 / 8 and 32 / 4 of 128 and 14 / 2 of 64, 1 to 16 sequences of 0 to 16000 tokens, 1 to
 // 2000 rows: the choice costs 0.5 % of the better kernel's time on average and 19 % at most.  few / many measured, bf16: heads 32 / 8, 1
 // sequence, 32 rows behind 8000 and 16000 tokens 20 / 25, 30 / 31, 200 rows behind 8000 82 / 46; 8 sequences, 8, 17 and 32 rows behind
@@ -182,7 +184,7 @@ inline Kv8Shares kv8_shares(long long items, long long tiles, int pages, int res
     const long long fill = std::max<long long>(KV8_WGS / std::max<long long>(items, 1), resident > 2 && items * 2 <= KV8_WGS / 2 * resident ? 2 : 1);
     return Kv8Shares{items, (int)std::max<long long>(1, std::min<long long>({fill, KV8_PART_TILES / std::max<long long>(tiles, 1), 32, (pages + 7) / 8}))};
 }
-inline double kv8_few_us(const Kv8Shares &s, double pages, int hd) { return 6.0 + 0.005 * (double)s.items * s.NS + 0.0012 * (double)s.items * pages * hd / 128; }
+inline double kv8_few_us(const Kv8Shares &s, double pages, int hd) { return 6.0 + 0.005 * (double)s.items * s.NS + 0.0012 * std::max<double>(s.items, (double)KV8_WGS / s.NS) * pages * hd / 128; }
 inline double kv8_many_us(const Kv8Shares &s, long long heads, int rt32, double pages, int hd, int planes) {
     return 10.0 + (0.0008 + (0.0002 + 0.0011 * planes) * rt32) * (double)heads * pages * hd / 128 + (s.NS > 1 ? 5.0 + 0.2 * s.NS : 0.0);
 }
