@@ -551,3 +551,38 @@ def test_two_caches_work_at_once():
             kv.close()
     for j in range(2):
         assert torch.equal(outs[True][j], outs[False][j])
+
+
+@pytest.mark.parametrize("heads,dtype", [((3, 3, 32), "bf16"), ((10, 2, 64), "f32"), ((64, 1, 128), "bf16"), ((192, 3, 32), "f32"), ((6, 1, 128), "f32")])
+def test_groups_that_fill_no_tile_and_groups_of_64(heads, dtype):
+    p = Pair(heads, 5, 512, max_rows=1200, dtype=dtype, seed=heads[0])
+    start = [0, 31, 130, 300, 64]
+    p.reserve([0] * 5, start)
+    p.append()
+    p.reserve(start, [1, 5, 33, 0, 2])
+    p.append()
+    p.attend()
+    p.reserve([130, 31, 0, 300, 66], [3, 0, 0, 70, 0], check=False)      # the first has too few tokens, the third leaves
+    p.append()
+    p.attend(scale=0.1)
+    p.kv.close()
+
+
+def test_a_thousand_sequences_and_ranges_of_keys_in_part_of_the_chip():
+    p = Pair((4, 2, 32), 1024, 128, n_pages=1500, max_rows=4096, seed=6)
+    start = [int(x) for x in p.rng.integers(0, 6, 1024)]
+    p.reserve([0] * 1024, start)
+    p.append()
+    p.reserve(start, [(b * 7) % 3 for b in range(1024)])
+    p.append()
+    p.attend()
+    p.kv.close()
+    for heads, dtype, batch, new in (((32, 8, 128), "bf16", 14, 12), ((14, 2, 64), "f32", 16, 21), ((32, 8, 128), "bf16", 3, 32)):
+        p = Pair(heads, batch, 2048, max_rows=20000, dtype=dtype, seed=batch)
+        start = [900 + 25 * b for b in range(batch)]
+        p.reserve([0] * batch, start)
+        p.append()
+        p.reserve(start, [new - b % 2 for b in range(batch)])
+        p.append()
+        p.attend(q_scale=2.0)
+        p.kv.close()
