@@ -25,6 +25,7 @@ namespace deer {
 
 constexpr int KV8_PAGE = 64, KV8_RING = 128, KV8_SLOTS = 192;   // slots of the ring, and with the kept page
 constexpr int KV8_MAX_BATCH = 1024;
+constexpr int KV8_SORT = 128;     // sequences that a pass puts in order
 
 struct Kv8State {      // device arrays
     int *table;        // [max_batch][max_blocks]: page of every 64 tokens, -1 beyond the pages held
@@ -36,6 +37,7 @@ struct Kv8State {      // device arrays
     int *start, *count, *hotbase;  // [max_batch]: first position, rows granted, see above
     int *carry;        // [max_batch]: where the open page's older rows are: 0 none, 1 the ring, 2 the kept page
     int *cu;           // [max_batch + 1]: first row of every sequence
+    int *order;        // [max_batch]: passes of up to KV8_SORT sequences: those with the most keys first
     int *slot, *row_seq, *row_pos; // [max_rows]
     int max_blocks, max_batch, n_pages, max_rows;
 };
@@ -79,7 +81,7 @@ __global__ void k_kv8_init(Kv8State s) {
     const size_t i = (size_t)blockIdx.x * blockDim.x + threadIdx.x, n = (size_t)gridDim.x * blockDim.x;
     for (size_t j = i; j < (size_t)s.max_batch * s.max_blocks; j += n) s.table[j] = -1;
     for (size_t j = i; j < (size_t)s.n_pages; j += n) s.free[j] = s.n_pages - 1 - (int)j;
-    for (size_t j = i; j < (size_t)s.max_batch; j += n) { s.len[j] = s.held[j] = s.hot[j] = s.base[j] = s.start[j] = s.count[j] = s.hotbase[j] = s.carry[j] = 0; }
+    for (size_t j = i; j < (size_t)s.max_batch; j += n) { s.len[j] = s.held[j] = s.hot[j] = s.base[j] = s.start[j] = s.count[j] = s.hotbase[j] = s.carry[j] = 0; s.order[j] = (int)j; }
     for (size_t j = i; j <= (size_t)s.max_batch; j += n) s.cu[j] = 0;
     for (size_t j = i; j < (size_t)s.max_rows; j += n) { s.slot[j] = -1; s.row_seq[j] = -1; s.row_pos[j] = 0; }
     if (i < 8) s.stat[i] = i == 0 ? s.n_pages : 0;
@@ -91,12 +93,13 @@ __global__ void k_kv8_init(Kv8State s) {
 // A sequence is refused (keeps its pages and tokens, gets no rows) for numbers out of range, a start behind its tokens, a start
 // inside a page whose bf16 rows are gone, or, like every growing one behind it, where the pages do not suffice.
 // Every workgroup works out all sequences (one scan) and writes its share of table entries and rows, four rows to a thread; the
-// state itself is written by the last to arrive, when all have read it (so that start may be the lengths themselves).  Bound by latency:
+// state itself is written by the last to arrive, when all have read it (so that start may be the lengths themselves), with the order of up
+// to 128 sequences by their keys, in which attention takes them.  Bound by latency:
 // 16 sequences 4 to 6 us, 1000 prompts with 512500 rows 13 us (their 6.1 MB would take 1).  grid: any; 1024 threads; B <= 1024.
 __global__ __launch_bounds__(1024) void k_kv8_reserve(Kv8State s, const int *start, int start_add, const int *__restrict__ count,
                                                       int count_const, int B, int rows, int max_new, int max_len, int scratch) {
     __shared__ int s_row[KV8_MAX_BATCH], s_start[KV8_MAX_BATCH], s_n[KV8_MAX_BATCH], s_held[KV8_MAX_BATCH], s_tp[KV8_MAX_BATCH],
-        s_grow[KV8_MAX_BATCH], s_give[KV8_MAX_BATCH], s_taken, s_given, s_refused, s_flag;
+        s_grow[KV8_MAX_BATCH], s_give[KV8_MAX_BATCH], s_keys[KV8_SORT], s_taken, s_given, s_refused, s_flag;
     __shared__ Kv8Sums tmp[16];
     const int b = threadIdx.x;
     int st = 0, n = 0, len = 0, held = 0, hot = 0, base = 0;
@@ -123,6 +126,7 @@ __global__ __launch_bounds__(1024) void k_kv8_reserve(Kv8State s, const int *sta
     if (grow > 0 && grow_end > avail) ok = false;
     const int m = ok ? n : 0, last = (st + max(m, 1) - 1) / KV8_PAGE;
     s_row[b] = b < B ? row0 : 0x7fffffff; s_start[b] = st; s_n[b] = m; s_held[b] = held; s_tp[b] = tp; s_grow[b] = grow_end; s_give[b] = give_end;
+    if (b < KV8_SORT) s_keys[b] = m > 0 ? st + m : 0;
     if (ok && grow > 0) atomicMax(&s_taken, grow_end);
     if (b < B && !ok) atomicAdd(&s_refused, 1);
     __syncthreads();
@@ -173,6 +177,12 @@ __global__ __launch_bounds__(1024) void k_kv8_reserve(Kv8State s, const int *sta
         s.start[b] = st; s.count[b] = m; s.cu[b] = min(row0, rows);
         s.hotbase[b] = scratch ? (touched_end - touched - first) * KV8_PAGE : 0;
         if (b == B - 1) s.cu[B] = min(row_end, rows);
+        if (B > 1 && B <= KV8_SORT) {
+            const int mine = s_keys[b];
+            int at = 0;
+            for (int j = 0; j < B; ++j) at += s_keys[j] > mine || (s_keys[j] == mine && j < b) ? 1 : 0;
+            s.order[at] = b;
+        }
         const int older = m > 0 && st % KV8_PAGE ? (in_ring ? 1 : 2) : 0;
         s.carry[b] = scratch || older == 2 ? older : 0;       // (a short pass finds the ring's rows where they are)
         if (ok) {
@@ -503,6 +513,7 @@ struct Kv8Attn {
     const uint4 *qhi, *qlo; uint4 *xhi, *xlo;      // fragments
     const int *q_row0;                             // fragments: attention row of a sequence's first row; null: 32 * sequence
     float *part; int *counters;                    // counters: zero between kernels
+    const int *order;                              // sequence of the grid's z, or null: z
     int Hq, Hkv, G, NS, rts;                       // NS key ranges; rts: tiles of packed rows per sequence
     float scale_log2e, m_init;
 };
@@ -548,6 +559,13 @@ __device__ __forceinline__ Kv8Row kv8_row(const Kv8Attn &a, int b, int kvh, int 
     r.h0 = warm ? own * KV8_PAGE : r.lim;
     r.lim8 = r.h0;
     return r;
+}
+
+// The sequence of a workgroup.  Workgroups that share a compute unit slow each other, and those of the longest sequences end last: they
+// start first, one to a unit (8 sequences of 618 to 2925 tokens in no order, 17 rows of heads 32 / 4 of 128: 25 -> 22 us;
+// 12 of 500 to 6000, 32 rows of 32 / 8 in float32 79 -> 70; 8 prompts of 300 behind 300 to 3000 105 -> 92; equal lengths as before).
+__device__ __forceinline__ int kv8_sequence(const Kv8Attn &a) {
+    return a.order ? (int)min((unsigned)a.order[blockIdx.z], gridDim.z - 1) : (int)blockIdx.z;
 }
 
 template <int HD, int SRC>
@@ -750,7 +768,7 @@ __global__ __launch_bounds__(256, (kv8_few_resident<HD, SRC>())) void k_kv8_attn
     __shared__ int s_flag;
     const int tidx = opaque_tid();
     const int w = __builtin_amdgcn_readfirstlane(tidx >> 6), lane = tidx & 63, n = lane & 15, g = lane >> 4;
-    const int b = blockIdx.z, rt = blockIdx.y, kvh = blockIdx.x % opaque_s(a.Hkv), split = blockIdx.x / opaque_s(a.Hkv);
+    const int b = kv8_sequence(a), rt = blockIdx.y, kvh = blockIdx.x % opaque_s(a.Hkv), split = blockIdx.x / opaque_s(a.Hkv);
     const int stride = W * a.NS;
     const int *table = a.s.table + (size_t)b * a.s.max_blocks;
     int u = split * W + w;
@@ -999,7 +1017,7 @@ __global__ __launch_bounds__(256, HD == 128 && SRC == KV8_F32 ? 1 : 2) void k_kv
     __shared__ int s_span[4][4];
     const int tidx = opaque_tid();
     const int w = __builtin_amdgcn_readfirstlane(tidx >> 6), lane = tidx & 63, half = lane >> 5;
-    const int b = blockIdx.z, rt0 = (gridDim.y - 1 - blockIdx.y) * 4, kvh = blockIdx.x % opaque_s(a.Hkv), split = blockIdx.x / opaque_s(a.Hkv);
+    const int b = kv8_sequence(a), rt0 = (gridDim.y - 1 - blockIdx.y) * 4, kvh = blockIdx.x % opaque_s(a.Hkv), split = blockIdx.x / opaque_s(a.Hkv);
     const int packed = (a.s.cu[b + 1] - a.s.cu[b]) * a.G;
     if (rt0 * 32 >= packed) return;
     const int rt = rt0 + w;

@@ -73,7 +73,7 @@ inline void plan_kv8(Kv8Cache &c, const Kv8Shape &p, char *cache, char *work) {
     s.stat = (int *)take(8 * 4);
     c.cache_bytes = off;
     off = 0; base = work;
-    s.start = (int *)take(p.max_batch * 4); s.count = (int *)take(p.max_batch * 4); s.hotbase = (int *)take(p.max_batch * 4); s.carry = (int *)take(p.max_batch * 4);
+    s.start = (int *)take(p.max_batch * 4); s.count = (int *)take(p.max_batch * 4); s.hotbase = (int *)take(p.max_batch * 4); s.carry = (int *)take(p.max_batch * 4); s.order = (int *)take(p.max_batch * 4);
     s.cu = (int *)take((p.max_batch + 1) * 4);
     c.ask_start = (int *)take(p.max_batch * 4); c.ask_count = (int *)take(p.max_batch * 4); c.ask_row0 = (int *)take(p.max_batch * 4);
     s.slot = (int *)take((size_t)p.max_rows * 4); s.row_seq = (int *)take((size_t)p.max_rows * 4); s.row_pos = (int *)take((size_t)p.max_rows * 4);
@@ -188,6 +188,8 @@ inline double kv8_few_us(const Kv8Shares &s, double pages, int hd) { return 6.0 
 inline double kv8_many_us(const Kv8Shares &s, long long heads, int rt32, double pages, int hd, int planes) {
     return 10.0 + (0.0008 + (0.0002 + 0.0011 * planes) * rt32) * (double)heads * pages * hd / 128 + (s.NS > 1 ? 5.0 + 0.2 * s.NS : 0.0);
 }
+// The sequences' order matters where workgroups share compute units.
+inline const int *kv8_order(const Kv8Cache &c, long long workgroups) { return c.batch > 1 && c.batch <= KV8_SORT && workgroups > KV8_WGS / 2 ? c.st.order : nullptr; }
 template <int HD, int SRC>
 hipError_t kv8_attend_src(Kv8Cache &c, hipStream_t s, Kv8Attn &a) {
     const int B = c.batch, packed = c.max_new * a.G, pages = (c.max_len + KV8_PAGE - 1) / KV8_PAGE;
@@ -197,13 +199,13 @@ hipError_t kv8_attend_src(Kv8Cache &c, hipStream_t s, Kv8Attn &a) {
     const Kv8Shares m = kv8_shares(heads * groups, heads * rt32, pages * 2, 2);      // (a workgroup of this kernel takes four pages at least)
     const double seen = (c.max_len - 0.5 * c.max_new) / KV8_PAGE + 0.5;
     if (kv8_few_us(f, seen, HD) <= kv8_many_us(m, heads, rt32, seen, HD, Kv8Planes<HD, SRC>::N) && rt16 <= 65535) {
-        a.rts = rt16; a.NS = f.NS;
+        a.rts = rt16; a.NS = f.NS; a.order = kv8_order(c, f.items * f.NS);
         const dim3 grid(a.Hkv * a.NS, rt16, B);
         if (rt16 == 1 && (double)c.p.n_layers * B * pages * c.page_bytes() > KV8_SIDE_CACHE) hipLaunchKernelGGL((k_kv8_attn_few<HD, SRC, true>), grid, dim3(256), 0, s, a);
         else hipLaunchKernelGGL((k_kv8_attn_few<HD, SRC, false>), grid, dim3(256), 0, s, a);
         return hipGetLastError();
     }
-    a.rts = rt32; a.NS = m.NS;
+    a.rts = rt32; a.NS = m.NS; a.order = kv8_order(c, m.items * m.NS);
     hipLaunchKernelGGL((k_kv8_attn_many<HD, SRC>), dim3(a.Hkv * a.NS, groups, B), dim3(256), 0, s, a);
     if (hipError_t e = hipGetLastError()) return e;
     if (a.NS > 1) hipLaunchKernelGGL((k_kv8_merge<HD, SRC>), dim3(a.Hkv, rt32, B), dim3(4 * HD), 0, s, a);

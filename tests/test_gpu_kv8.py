@@ -586,3 +586,15 @@ def test_a_thousand_sequences_and_ranges_of_keys_in_part_of_the_chip():
         p.append()
         p.attend(q_scale=2.0)
         p.kv.close()
+
+
+@pytest.mark.parametrize("batch", [2, 127, 128, 129])
+def test_sequences_of_equal_and_unequal_lengths_in_any_order(batch):
+    p = Pair((14, 2, 64), batch, 512, max_rows=40 * batch if batch > 2 else 1000, seed=batch)
+    start = [int(x) for x in p.rng.choice([0, 1, 7, 7, 35], batch)] if batch > 2 else [30, 330]
+    p.reserve([0] * batch, start)
+    p.append()
+    p.reserve(start, [int(x) for x in p.rng.choice([0, 1, 3, 3], batch)] if batch > 2 else [150, 150])
+    p.append()
+    p.attend()
+    p.kv.close()
